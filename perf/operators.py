@@ -197,7 +197,7 @@ def _norm_grad(c, r, g, norm):
 
 def _plain_norm_bwd(s):
     case, rows, dt = s["case"], s["rows"].long(), s["dR"].dtype
-    dR, dZ = s["dR"].float(), s["dZ"].float()
+    dR, dZ = s["dR"].to(torch.float32, copy=True), s["dZ"].float()       # (the gradient is written over below)
     c, r = _statistics(s["R"].float(), case["norm"])
     G = dR[rows] + _norm_grad(c, r, dZ * s["pre_w"], case["norm"])
     out = {"dpre_w": (dZ * (c * r)).sum(0), "dpre_b": dZ.sum(0) if s["pre_b"] is not None else None}
