@@ -15,6 +15,7 @@
  *   sbp_attention_backward  dQ, dK, dV of attention on the kept tokens (Sec. 4, Drop QKV / Drop Query only)
  *   sbp_act_backward     dZ = dH * gelu'(Z_keep) on packed rows between two layers of a block (Sec. 3.3.1)
  *   sbp_patch_cache / sbp_patch_scatter  stride >= kernel convolutions as linear layers on patch rows (Sec. 3.2.2)
+ *   sbp_block_norm_forward / _backward  norms before and after a block with its gate and residual scale
  *
  * Nothing is rescaled by 1/r: Eq. 1 keeps the plain 1/B factor.
  *
@@ -56,6 +57,12 @@ typedef enum { SBP_F32 = 0, SBP_BF16 = 1 } sbp_dtype;
 
 /* position-wise activations sbp_act_backward knows */
 typedef enum { SBP_ACT_GELU = 0 /* exact form: z Phi(z) */ } sbp_activation;
+
+/* row norms sbp_block_norm_forward / _backward know, over the C channels of a row */
+typedef enum {
+    SBP_NORM_LAYER = 0, /* (x - mean) / sqrt(var + eps), var = mean((x - mean)^2) */
+    SBP_NORM_RMS = 1    /* x / sqrt(mean(x^2) + eps) */
+} sbp_norm;
 
 /* Sec. 4, "How to sample the gradient keep mask?": uniformly random positions,
  * or a structured periodic ("grid-wise") mask. */
@@ -262,6 +269,71 @@ int sbp_linear_backward_kernel_count(sbp_dtype dt, int64_t M, int64_t M_keep_cap
 sbp_status sbp_act_backward(sbp_dtype dt, sbp_activation act, const void* Z_keep /* dev */, const void* dH /* dev */,
                             const int32_t* M_keep_dev /* dev, nullable */, int64_t M_keep_cap, int64_t C,
                             void* dZ /* dev */, int32_t* status_word /* dev, nullable */, void* stream);
+
+/*
+ * The residual stream between two blocks in one pass: the norm after a block, the block's gate, the residual addition and
+ * the norm in front of the next block, on every row, with the rows that the backward pass needs cached for the kept ones
+ * (Algorithm 1: every row is computed, only kept rows are retained):
+ *   u_m = N(Y_m) * post_w + post_b      (post_w NULL: u = Y)
+ *   R_m = residual_scale * H_m + gate[m / gate_group] * u_m        (gate NULL: 1)
+ *   Z_m = N(R_m) * pre_w + pre_b        (pre_w NULL: no Z)
+ * H [M, C] the residual stream, Y [M, C] the block's output; either may be NULL (taken as zeros), not both.  gate
+ * [ceil(M / gate_group), C] in dt: one row for each gate_group consecutive rows - 1 a gate for each token, N for each
+ * sample, M a scale for each channel.  Norm weights and biases fp32 [C], biases nullable.  residual_scale and eps > 0 or 0.
+ * Outputs: R [M, C] (nullable; may be H or Y), Z [M, C] (nullable), and the packed rows Y_keep, R_keep, Z_keep
+ * [M_keep_cap, C] (each nullable) of Y, R and Z with the rows past M_keep cleared: R_keep and Y_keep are what
+ * sbp_block_norm_backward reads, Z_keep is the X_keep of the linear layer behind the norm.  keep_rows strictly ascending,
+ * as sbp_sample_keep writes them; NULL: rows 0 .. M_keep - 1.  M_keep as for sbp_forward_cache.
+ * No buffer overlaps another, but for R.  Statistics and sums in fp32; R is normalised before it is rounded; one rounding
+ * to dt of each output.
+ * SBP_ERR_UNSUPPORTED: C * sizeof(element) not a multiple of 16, C > 8192.  SBP_ERR_INVALID_ARG for null / misaligned (16
+ * bytes) pointers, bad sizes, a post_b or pre_b without its weight, Z or Z_keep without pre_w, post_w, gate or Y_keep
+ * without Y, and scales or eps that are not finite (eps also: negative).
+ */
+sbp_status sbp_block_norm_forward(sbp_dtype dt, sbp_norm norm, const void* H /* dev, nullable */, const void* Y /* dev, nullable */,
+                                  const float* post_w /* dev, nullable */, const float* post_b /* dev, nullable */,
+                                  const void* gate /* dev, nullable */, int64_t gate_group, double residual_scale,
+                                  const float* pre_w /* dev, nullable */, const float* pre_b /* dev, nullable */, double eps,
+                                  int64_t M, int64_t C, void* R /* dev, nullable */, void* Z /* dev, nullable */,
+                                  const int32_t* keep_rows /* dev, nullable */, const int32_t* M_keep_dev /* dev, nullable */,
+                                  int64_t M_keep_cap, void* Y_keep /* dev, nullable */, void* R_keep /* dev, nullable */,
+                                  void* Z_keep /* dev, nullable */, int32_t* status_word /* dev, nullable */, void* stream);
+
+/* Scratch bytes sbp_block_norm_backward needs for these sizes (never 0): partial sums of the weights' gradients. */
+size_t sbp_block_norm_backward_workspace_bytes(sbp_dtype dt, int64_t M, int64_t M_keep_cap, int64_t C);
+
+/*
+ * Backward of sbp_block_norm_forward with the gradients of Z and of the block's output kept on the kept rows; the residual
+ * stream's own gradient passes on every row.  With n the normalised row and r its 1 / sqrt(...), norm'(q) =
+ * r (q - mean(q) - n mean(q n)), without mean(q) for SBP_NORM_RMS.  For kept row m (of the list), row k = keep_rows[m]:
+ *   G_m   = dR[k] + norm'(dZ_m * pre_w) at R_keep_m
+ *   dH[k] = residual_scale * G_m                    every other row of dH = residual_scale * dR
+ *   dY_m  = norm'(gate * G_m * post_w) at Y_keep_m  (post_w NULL: gate * G_m)
+ *   dpre_w = sum dZ n_R,  dpre_b = sum dZ,  dgate[j] = sum over kept rows k / gate_group = j of G u,
+ *   dpost_w = sum gate G n_Y,  dpost_b = sum gate G
+ * dR, dH [M, C]; dZ, R_keep, Y_keep, dY packed [M_keep_cap, C] (dZ is the SBP_FLAG_DX_COMPACT output of the linear layer
+ * behind the norm, dY the SBP_FLAG_DY_COMPACT input of the block's last one); rows of dY past M_keep are cleared.  Weight
+ * gradients fp32.  dR NULL: zero (the stream ends here); dZ NULL: no gradient from a norm behind.  Every output is nullable.
+ * dH may be dR and dY may be dZ or Y_keep; otherwise no buffer overlaps another.  A stream that is itself kept packed is a
+ * call with keep_rows NULL and M = M_keep_cap.  keep_rows strictly ascending; entries outside [0, M) are skipped.
+ * Arguments as in the forward call (pre_b does not matter here).  flags: SBP_FLAG_ACCUMULATE adds into the five weight gradients;
+ * SBP_FLAG_VALIDATE checks keep_rows first, as in sbp_linear_backward.  workspace: 256-byte aligned.  Statistics are made
+ * again from R_keep and Y_keep, in fp32; sums are fp32, added in a fixed order.
+ * SBP_ERR_UNSUPPORTED as in the forward call.  SBP_ERR_INVALID_ARG also for dZ without R_keep and pre_w, dpre_* without
+ * dZ, dpost_* without post_w and Y_keep, dgate without gate and Y_keep, dY with post_w and without Y_keep, dR and dZ both
+ * NULL.  SBP_ERR_WORKSPACE as for sbp_linear_backward (no workspace is needed when no weight gradient is wanted).
+ */
+sbp_status sbp_block_norm_backward(sbp_dtype dt, sbp_norm norm, const void* dR /* dev, nullable */, const void* dZ /* dev, nullable */,
+                                   const void* R_keep /* dev, nullable */, const void* Y_keep /* dev, nullable */,
+                                   const float* post_w /* dev, nullable */, const float* post_b /* dev, nullable */,
+                                   const void* gate /* dev, nullable */, int64_t gate_group, double residual_scale,
+                                   const float* pre_w /* dev, nullable */, double eps,
+                                   const int32_t* keep_rows /* dev, nullable */, const int32_t* M_keep_dev /* dev, nullable */,
+                                   int64_t M, int64_t M_keep_cap, int64_t C, void* dH /* dev, nullable */, void* dY /* dev, nullable */,
+                                   float* dpost_w /* dev, nullable */, float* dpost_b /* dev, nullable */,
+                                   float* dgate /* dev, nullable */, float* dpre_w /* dev, nullable */,
+                                   float* dpre_b /* dev, nullable */, uint32_t flags, void* workspace /* dev */,
+                                   size_t workspace_bytes, int32_t* status_word /* dev, nullable */, void* stream);
 
 /*
  * Convolutions with stride >= kernel size as SBP layers (Sec. 3.2.2, the text after Eq. 6: with s >= k the

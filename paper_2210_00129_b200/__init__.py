@@ -26,6 +26,7 @@ SBP_OK, SBP_ERR_INVALID_ARG, SBP_ERR_UNSUPPORTED, SBP_ERR_WORKSPACE = 0, 1, 2, 3
 SBP_ERR_CUDA, SBP_ERR_TIMEOUT, SBP_ERR_BAD_INDICES = 4, 5, 6
 SBP_F32, SBP_BF16 = 0, 1
 SBP_ACT_GELU = 0
+SBP_NORM_LAYER, SBP_NORM_RMS = 0, 1
 SBP_MASK_RANDOM, SBP_MASK_GRID, SBP_MASK_TEMPORAL, SBP_MASK_TEMPORAL_GRID = 0, 1, 2, 3
 SBP_FLAG_SHARE_MASK, SBP_FLAG_ACCUMULATE, SBP_FLAG_VALIDATE, SBP_FLAG_PLAIN_FMA = 1, 2, 4, 8
 SBP_FLAG_DY_COMPACT, SBP_FLAG_DX_COMPACT, SBP_FLAG_W_OUT_IN, SBP_FLAG_ATTN_ALL_KEYS = 16, 32, 64, 128
@@ -33,7 +34,8 @@ SBP_FLAG_ATTN_KEPT_ROWS_ONLY = 256
 
 EXPORTS = ("sbp_status_string", "sbp_keep_count", "sbp_sample_keep", "sbp_forward_cache", "sbp_linear_forward",
            "sbp_linear_backward_workspace_bytes", "sbp_linear_backward", "sbp_linear_backward_kernel_count",
-           "sbp_plan_search_count", "sbp_act_backward", "sbp_attention_backward", "sbp_patch_cache", "sbp_patch_scatter_workspace_bytes",
+           "sbp_plan_search_count", "sbp_act_backward", "sbp_block_norm_forward",
+           "sbp_block_norm_backward_workspace_bytes", "sbp_block_norm_backward", "sbp_attention_backward", "sbp_patch_cache", "sbp_patch_scatter_workspace_bytes",
            "sbp_patch_scatter", "sbp_step_host_arena_bytes", "sbp_step_host", "sbp_bias_grad_static",
            "sbp_selftest_bounded_wait", "sbp_probe_gather_ring", "sbp_probe_mma_rate", "sbp_probe_mma_pair_rate", "sbp_probe_operand_feed")
 
@@ -95,6 +97,14 @@ def load_library() -> ctypes.CDLL:
     lib.sbp_probe_mma_pair_rate.restype = ci
     lib.sbp_act_backward.argtypes = [ci, ci, vp, vp, vp, i64, i64, vp, vp, vp]
     lib.sbp_act_backward.restype = ci
+    lib.sbp_block_norm_forward.argtypes = [ci, ci, vp, vp, vp, vp, vp, i64, dbl, vp, vp, dbl, i64, i64, vp, vp, vp, vp, i64, vp, vp, vp,
+                                           vp, vp]
+    lib.sbp_block_norm_forward.restype = ci
+    lib.sbp_block_norm_backward_workspace_bytes.argtypes = [ci, i64, i64, i64]
+    lib.sbp_block_norm_backward_workspace_bytes.restype = sz
+    lib.sbp_block_norm_backward.argtypes = [ci, ci, vp, vp, vp, vp, vp, vp, vp, i64, dbl, vp, dbl, vp, vp, i64, i64, i64, vp, vp, vp, vp,
+                                            vp, vp, vp, u32, vp, sz, vp, vp]
+    lib.sbp_block_norm_backward.restype = ci
     lib.sbp_plan_search_count.argtypes = []
     lib.sbp_plan_search_count.restype = i64
     lib.sbp_step_host_arena_bytes.argtypes = [ci, ci, i64, i64, i64, i64, i64, dbl]
@@ -266,6 +276,33 @@ def sbp_act_backward(dt, act, Z_keep, dH, M_keep_dev, M_keep_cap, C, dZ, status_
     s = _calls().sbp_act_backward(dt, act, Z_keep, dH, M_keep_dev, M_keep_cap, C, dZ, status_word, _stream(stream))
     if check:
         _check(s, "sbp_act_backward")
+    return s
+
+
+def sbp_block_norm_forward(dt, norm, H, Y, post_w, post_b, gate, gate_group, residual_scale, pre_w, pre_b, eps, M, C, R, Z,
+                           keep_rows=None, M_keep_dev=None, M_keep_cap=0, Y_keep=None, R_keep=None, Z_keep=None, status_word=None,
+                           stream=None, check=True) -> int:
+    """R = residual_scale H + gate norm(Y), Z = norm(R), with the kept rows of Y, R and Z cached by the same launch."""
+    s = _calls().sbp_block_norm_forward(dt, norm, H, Y, post_w, post_b, gate, gate_group, residual_scale, pre_w, pre_b, eps, M, C, R,
+                                        Z, keep_rows, M_keep_dev, M_keep_cap, Y_keep, R_keep, Z_keep, status_word, _stream(stream))
+    if check:
+        _check(s, "sbp_block_norm_forward")
+    return s
+
+
+def sbp_block_norm_backward_workspace_bytes(dt, M, M_keep_cap, C) -> int:
+    return int(load_library().sbp_block_norm_backward_workspace_bytes(dt, M, M_keep_cap, C))
+
+
+def sbp_block_norm_backward(dt, norm, dR, dZ, R_keep, Y_keep, post_w, post_b, gate, gate_group, residual_scale, pre_w, eps, keep_rows,
+                            M_keep_dev, M, M_keep_cap, C, dH, dY, dpost_w, dpost_b, dgate, dpre_w, dpre_b, flags, workspace,
+                            workspace_bytes, status_word=None, stream=None, check=True) -> int:
+    """Gradients of sbp_block_norm_forward: dH on every row, dY packed, fp32 gradients of the norms' weights and of the gate."""
+    s = _calls().sbp_block_norm_backward(dt, norm, dR, dZ, R_keep, Y_keep, post_w, post_b, gate, gate_group, residual_scale, pre_w, eps,
+                                         keep_rows, M_keep_dev, M, M_keep_cap, C, dH, dY, dpost_w, dpost_b, dgate, dpre_w, dpre_b,
+                                         flags, workspace, workspace_bytes, status_word, _stream(stream))
+    if check:
+        _check(s, "sbp_block_norm_backward")
     return s
 
 

@@ -100,6 +100,8 @@ PyMethodDef g_methods[] = {
     SBP_CALL(sbp_linear_backward),
     SBP_CALL(sbp_attention_backward),
     SBP_CALL(sbp_act_backward),
+    SBP_CALL(sbp_block_norm_forward),
+    SBP_CALL(sbp_block_norm_backward),
     SBP_CALL(sbp_patch_cache),
     SBP_CALL(sbp_patch_scatter),
     SBP_CALL(sbp_step_host),

@@ -366,6 +366,81 @@ sbp_status sbp_act_backward(sbp_dtype dt, sbp_activation act, const void* Z_keep
 }
 
 namespace {
+// shared argument checks of the two norm calls
+sbp_status norm_arguments(sbp_dtype dt, sbp_norm norm, const void* gate, int64_t gate_group, double scale, double eps, int64_t M,
+                          int64_t M_keep_cap, int64_t C, const int32_t* keep_rows, const int32_t* M_keep_dev) {
+    if (dt != SBP_F32 && dt != SBP_BF16) return SBP_ERR_INVALID_ARG;
+    if (norm != SBP_NORM_LAYER && norm != SBP_NORM_RMS) return SBP_ERR_INVALID_ARG;
+    if (M <= 0 || M >= (1ll << 31) || C <= 0 || C >= (1ll << 24) || M_keep_cap < 0 || M_keep_cap > M) return SBP_ERR_INVALID_ARG;
+    if (gate != nullptr && gate_group <= 0) return SBP_ERR_INVALID_ARG;
+    if (!isfinite(scale) || !isfinite((float)scale) || !(eps >= 0.0) || !isfinite((float)eps)) return SBP_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(keep_rows) & 3u) || (reinterpret_cast<uintptr_t>(M_keep_dev) & 3u)) return SBP_ERR_INVALID_ARG;
+    if ((C * (dt == SBP_BF16 ? 2 : 4)) % 16 != 0 || C > block_norm_max_channels()) return SBP_ERR_UNSUPPORTED;
+    return SBP_OK;
+}
+}  // namespace
+
+sbp_status sbp_block_norm_forward(sbp_dtype dt, sbp_norm norm, const void* H, const void* Y, const float* post_w, const float* post_b,
+                                  const void* gate, int64_t gate_group, double residual_scale, const float* pre_w, const float* pre_b,
+                                  double eps, int64_t M, int64_t C, void* R, void* Z, const int32_t* keep_rows, const int32_t* M_keep_dev,
+                                  int64_t M_keep_cap, void* Y_keep, void* R_keep, void* Z_keep, int32_t* status_word, void* stream) {
+    const sbp_status s = norm_arguments(dt, norm, gate, gate_group, residual_scale, eps, M, M_keep_cap, C, keep_rows, M_keep_dev);
+    if (s == SBP_ERR_INVALID_ARG) return s;
+    for (const void* q : {H, Y, (const void*)post_w, (const void*)post_b, gate, (const void*)pre_w, (const void*)pre_b, (const void*)R,
+                          (const void*)Z, (const void*)Y_keep, (const void*)R_keep, (const void*)Z_keep})
+        if (!aligned16(q)) return SBP_ERR_INVALID_ARG;
+    if (H == nullptr && Y == nullptr) return SBP_ERR_INVALID_ARG;
+    if (Y == nullptr && (post_w != nullptr || gate != nullptr || Y_keep != nullptr)) return SBP_ERR_INVALID_ARG;
+    if ((post_b != nullptr && post_w == nullptr) || (pre_b != nullptr && pre_w == nullptr)) return SBP_ERR_INVALID_ARG;
+    if (pre_w == nullptr && (Z != nullptr || Z_keep != nullptr)) return SBP_ERR_INVALID_ARG;
+    if (s != SBP_OK) return s;
+    const cudaError_t e = launch_block_norm_forward(dt, norm == SBP_NORM_LAYER, H, Y, post_w, post_b, gate, gate_group, (float)residual_scale,
+                                                    pre_w, pre_b, (float)eps, M, C, R, Z, keep_rows, M_keep_dev, M_keep_cap, Y_keep,
+                                                    R_keep, Z_keep, status_word, (cudaStream_t)stream);
+    return e == cudaSuccess ? SBP_OK : SBP_ERR_CUDA;
+}
+
+size_t sbp_block_norm_backward_workspace_bytes(sbp_dtype dt, int64_t M, int64_t M_keep_cap, int64_t C) {
+    if ((dt != SBP_F32 && dt != SBP_BF16) || M <= 0 || M_keep_cap < 0 || M_keep_cap > M || C <= 0 || C > block_norm_max_channels()) return 256;
+    return align_up(block_norm_backward_workspace_bytes(dt, M_keep_cap, C), 256);
+}
+
+sbp_status sbp_block_norm_backward(sbp_dtype dt, sbp_norm norm, const void* dR, const void* dZ, const void* R_keep, const void* Y_keep,
+                                   const float* post_w, const float* post_b, const void* gate, int64_t gate_group, double residual_scale,
+                                   const float* pre_w, double eps, const int32_t* keep_rows, const int32_t* M_keep_dev, int64_t M,
+                                   int64_t M_keep_cap, int64_t C, void* dH, void* dY, float* dpost_w, float* dpost_b, float* dgate,
+                                   float* dpre_w, float* dpre_b, uint32_t flags, void* workspace, size_t workspace_bytes,
+                                   int32_t* status_word, void* stream_v) {
+    cudaStream_t stream = (cudaStream_t)stream_v;
+    const sbp_status s = norm_arguments(dt, norm, gate, gate_group, residual_scale, eps, M, M_keep_cap, C, keep_rows, M_keep_dev);
+    if (s == SBP_ERR_INVALID_ARG) return s;
+    for (const void* q : {dR, dZ, R_keep, Y_keep, (const void*)post_w, (const void*)post_b, gate, (const void*)pre_w, (const void*)dH,
+                          (const void*)dY, (const void*)dpost_w, (const void*)dpost_b, (const void*)dgate, (const void*)dpre_w, (const void*)dpre_b})
+        if (!aligned16(q)) return SBP_ERR_INVALID_ARG;
+    if (dR == nullptr && dZ == nullptr) return SBP_ERR_INVALID_ARG;
+    if (dZ != nullptr && (R_keep == nullptr || pre_w == nullptr)) return SBP_ERR_INVALID_ARG;
+    if (dZ == nullptr && (dpre_w != nullptr || dpre_b != nullptr)) return SBP_ERR_INVALID_ARG;
+    if (post_b != nullptr && post_w == nullptr) return SBP_ERR_INVALID_ARG;
+    if ((dpost_w != nullptr || dpost_b != nullptr) && (post_w == nullptr || Y_keep == nullptr)) return SBP_ERR_INVALID_ARG;
+    if (dgate != nullptr && (gate == nullptr || Y_keep == nullptr)) return SBP_ERR_INVALID_ARG;
+    if (dY != nullptr && post_w != nullptr && Y_keep == nullptr) return SBP_ERR_INVALID_ARG;
+    if ((flags & SBP_FLAG_VALIDATE) && (status_word == nullptr || keep_rows == nullptr)) return SBP_ERR_INVALID_ARG;
+    if (s != SBP_OK) return s;
+    const bool sums = dpost_w != nullptr || dpost_b != nullptr || dgate != nullptr || dpre_w != nullptr || dpre_b != nullptr;
+    if (sums && (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
+                 workspace_bytes < sbp_block_norm_backward_workspace_bytes(dt, M, M_keep_cap, C)))
+        return SBP_ERR_WORKSPACE;
+    if (flags & SBP_FLAG_VALIDATE) {
+        if (launch_validate_keep_rows(keep_rows, M_keep_dev, M_keep_cap, M, status_word, stream) != cudaSuccess) return SBP_ERR_CUDA;
+    }
+    const cudaError_t e = launch_block_norm_backward(dt, norm == SBP_NORM_LAYER, dR, dZ, R_keep, Y_keep, post_w, post_b, gate, gate_group,
+                                                     (float)residual_scale, pre_w, (float)eps, keep_rows, M_keep_dev, M, M_keep_cap, C, dH,
+                                                     dY, dpost_w, dpost_b, dgate, dpre_w, dpre_b, (flags & SBP_FLAG_ACCUMULATE) != 0,
+                                                     static_cast<float*>(workspace), status_word, stream);
+    return e == cudaSuccess ? SBP_OK : SBP_ERR_CUDA;
+}
+
+namespace {
 // shared argument checks of the two patch calls; returns SBP_OK and the output grid when the geometry is usable
 sbp_status patch_geometry(sbp_dtype dt, int64_t B, int64_t H, int64_t W, int64_t C, int64_t k, int64_t stride, int64_t M_keep_cap,
                           int64_t* Ho, int64_t* Wo) {

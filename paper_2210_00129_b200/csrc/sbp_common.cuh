@@ -206,6 +206,21 @@ sbp_status launch_tc_forward(const void* X, const void* W, bool w_out_in, const 
 cudaError_t launch_act_backward(sbp_dtype dt, const void* Z, const void* dH, void* dZ, int64_t row_bytes, const int32_t* M_keep_dev,
                                 int64_t M_keep_cap, const int32_t* status_word, cudaStream_t stream);
 
+// norms before and after a block with its gate and residual scale (block_norm.cu)
+int64_t block_norm_max_channels();
+cudaError_t launch_block_norm_forward(sbp_dtype dt, bool layer, const void* H, const void* Y, const float* post_w, const float* post_b,
+                                      const void* gate, int64_t gate_group, float scale, const float* pre_w, const float* pre_b, float eps,
+                                      int64_t M, int64_t C, void* R, void* Z, const int32_t* keep_rows, const int32_t* M_keep_dev,
+                                      int64_t M_keep_cap, void* Y_keep, void* R_keep, void* Z_keep, const int32_t* status_word,
+                                      cudaStream_t stream);
+size_t block_norm_backward_workspace_bytes(sbp_dtype dt, int64_t M_keep_cap, int64_t C);
+cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR, const void* dZ, const void* R_keep, const void* Y_keep,
+                                       const float* post_w, const float* post_b, const void* gate, int64_t gate_group, float scale,
+                                       const float* pre_w, float eps, const int32_t* keep_rows, const int32_t* M_keep_dev, int64_t M,
+                                       int64_t M_keep_cap, int64_t C, void* dH, void* dY, float* dpost_w, float* dpost_b, float* dgate,
+                                       float* dpre_w, float* dpre_b, bool accumulate, float* workspace, const int32_t* status_word,
+                                       cudaStream_t stream);
+
 // stride >= kernel convolutions as linear layers on patch rows: gather of the kept patches, scatter of their gradients
 cudaError_t launch_patch_gather(const void* X, int64_t H, int64_t W, int64_t pos_bytes, int64_t k, int64_t s,
                                 const int32_t* keep_rows, const int32_t* M_keep_dev, int64_t M_keep_cap, void* X_keep,
