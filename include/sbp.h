@@ -16,6 +16,7 @@
  *   sbp_act_backward     dZ = dH * gelu'(Z_keep) on packed rows between two layers of a block (Sec. 3.3.1)
  *   sbp_patch_cache / sbp_patch_scatter  stride >= kernel convolutions as linear layers on patch rows (Sec. 3.2.2)
  *   sbp_block_norm_forward / _backward  norms before and after a block with its gate and residual scale
+ *   sbp_embedding_forward / _backward   rows of a table by id; the table's gradient from the kept rows
  *
  * Nothing is rescaled by 1/r: Eq. 1 keeps the plain 1/B factor.
  *
@@ -334,6 +335,36 @@ sbp_status sbp_block_norm_backward(sbp_dtype dt, sbp_norm norm, const void* dR /
                                    float* dgate /* dev, nullable */, float* dpre_w /* dev, nullable */,
                                    float* dpre_b /* dev, nullable */, uint32_t flags, void* workspace /* dev */,
                                    size_t workspace_bytes, int32_t* status_word /* dev, nullable */, void* stream);
+
+/*
+ * Where the residual stream starts: rows of a table by id - token embeddings, position tables -
+ *   out[m, :] = scale * table[ids[m], :] + add[m, :]         add [M, C] nullable (then + 0); out may be add
+ * table [V, C], add, out [M, C] in dt, ids int32 [M].  A negative id means no row (padding: out = add, or zero).  An id of V
+ * or more is reported as SBP_ERR_BAD_INDICES in the status word and taken as no row.  fp32 arithmetic, one rounding to dt.
+ * C * sizeof(element) must be a multiple of 16 (else SBP_ERR_UNSUPPORTED).  The other buffers do not overlap out.
+ */
+sbp_status sbp_embedding_forward(sbp_dtype dt, const void* table /* dev */, int64_t V, int64_t C, const int32_t* ids /* dev */,
+                                 int64_t M, double scale, const void* add /* dev, nullable */, void* out /* dev */,
+                                 int32_t* status_word /* dev, nullable */, void* stream);
+
+/* Scratch bytes sbp_embedding_backward needs for these sizes (never 0): the sorted list and partial rows. */
+size_t sbp_embedding_backward_workspace_bytes(sbp_dtype dt, int64_t M_keep_cap, int64_t V, int64_t C);
+
+/*
+ * Gradient of the table, with the gradient kept on the kept rows (the rows the stream's gradient was dropped from add nothing):
+ *   dTable[v, :] = scale * sum of dOut[k, :] over the kept rows k = keep_rows[m] with ids[k] = v         fp32 [V, C]
+ * Rows of dTable without such a k are zero.  dOut [M, C] in dt (with SBP_FLAG_DY_COMPACT packed, [M_keep_cap, C]: row m is
+ * the gradient of row keep_rows[m]); keep_rows NULL: rows 0 .. M_keep - 1.  M_keep as for sbp_forward_cache.  keep_rows in any
+ * order; entries outside [0, M) are skipped.  Negative ids add nothing, ids of V or more are reported and add nothing.
+ * Sums are fp32, each id's rows added in an order that depends on the sizes and the list alone: the same bits every time.
+ * flags: SBP_FLAG_ACCUMULATE adds into dTable (rows without a k are not touched), SBP_FLAG_DY_COMPACT.
+ * workspace: 256-byte aligned; SBP_ERR_WORKSPACE if short.  V < 2^31, C as in the forward call.
+ */
+sbp_status sbp_embedding_backward(sbp_dtype dt, const void* dOut /* dev */, const int32_t* ids /* dev */,
+                                  const int32_t* keep_rows /* dev, nullable */, const int32_t* M_keep_dev /* dev, nullable */,
+                                  int64_t M, int64_t M_keep_cap, int64_t V, int64_t C, double scale, float* dTable /* dev */,
+                                  uint32_t flags, void* workspace /* dev */, size_t workspace_bytes,
+                                  int32_t* status_word /* dev, nullable */, void* stream);
 
 /*
  * Convolutions with stride >= kernel size as SBP layers (Sec. 3.2.2, the text after Eq. 6: with s >= k the

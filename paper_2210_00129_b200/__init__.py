@@ -35,7 +35,8 @@ SBP_FLAG_ATTN_KEPT_ROWS_ONLY = 256
 EXPORTS = ("sbp_status_string", "sbp_keep_count", "sbp_sample_keep", "sbp_forward_cache", "sbp_linear_forward",
            "sbp_linear_backward_workspace_bytes", "sbp_linear_backward", "sbp_linear_backward_kernel_count",
            "sbp_plan_search_count", "sbp_act_backward", "sbp_block_norm_forward",
-           "sbp_block_norm_backward_workspace_bytes", "sbp_block_norm_backward", "sbp_attention_backward", "sbp_patch_cache", "sbp_patch_scatter_workspace_bytes",
+           "sbp_block_norm_backward_workspace_bytes", "sbp_block_norm_backward", "sbp_embedding_forward",
+           "sbp_embedding_backward_workspace_bytes", "sbp_embedding_backward", "sbp_attention_backward", "sbp_patch_cache", "sbp_patch_scatter_workspace_bytes",
            "sbp_patch_scatter", "sbp_step_host_arena_bytes", "sbp_step_host", "sbp_bias_grad_static",
            "sbp_selftest_bounded_wait", "sbp_probe_gather_ring", "sbp_probe_mma_rate", "sbp_probe_mma_pair_rate", "sbp_probe_operand_feed")
 
@@ -105,6 +106,12 @@ def load_library() -> ctypes.CDLL:
     lib.sbp_block_norm_backward.argtypes = [ci, ci, vp, vp, vp, vp, vp, vp, vp, i64, dbl, vp, dbl, vp, vp, i64, i64, i64, vp, vp, vp, vp,
                                             vp, vp, vp, u32, vp, sz, vp, vp]
     lib.sbp_block_norm_backward.restype = ci
+    lib.sbp_embedding_forward.argtypes = [ci, vp, i64, i64, vp, i64, dbl, vp, vp, vp, vp]
+    lib.sbp_embedding_forward.restype = ci
+    lib.sbp_embedding_backward_workspace_bytes.argtypes = [ci, i64, i64, i64]
+    lib.sbp_embedding_backward_workspace_bytes.restype = sz
+    lib.sbp_embedding_backward.argtypes = [ci, vp, vp, vp, vp, i64, i64, i64, i64, dbl, vp, u32, vp, sz, vp, vp]
+    lib.sbp_embedding_backward.restype = ci
     lib.sbp_plan_search_count.argtypes = []
     lib.sbp_plan_search_count.restype = i64
     lib.sbp_step_host_arena_bytes.argtypes = [ci, ci, i64, i64, i64, i64, i64, dbl]
@@ -303,6 +310,28 @@ def sbp_block_norm_backward(dt, norm, dR, dZ, R_keep, Y_keep, post_w, post_b, ga
                                          flags, workspace, workspace_bytes, status_word, _stream(stream))
     if check:
         _check(s, "sbp_block_norm_backward")
+    return s
+
+
+def sbp_embedding_forward(dt, table, V, C, ids, M, scale, add, out, status_word=None, stream=None, check=True) -> int:
+    """out = scale * table[ids] + add (negative ids: no row)."""
+    s = _calls().sbp_embedding_forward(dt, table, V, C, ids, M, scale, add, out, status_word, _stream(stream))
+    if check:
+        _check(s, "sbp_embedding_forward")
+    return s
+
+
+def sbp_embedding_backward_workspace_bytes(dt, M_keep_cap, V, C) -> int:
+    return int(load_library().sbp_embedding_backward_workspace_bytes(dt, M_keep_cap, V, C))
+
+
+def sbp_embedding_backward(dt, dOut, ids, keep_rows, M_keep_dev, M, M_keep_cap, V, C, scale, dTable, flags, workspace,
+                           workspace_bytes, status_word=None, stream=None, check=True) -> int:
+    """fp32 gradient of the table from the kept rows, summed by sorted ids."""
+    s = _calls().sbp_embedding_backward(dt, dOut, ids, keep_rows, M_keep_dev, M, M_keep_cap, V, C, scale, dTable, flags, workspace,
+                                        workspace_bytes, status_word, _stream(stream))
+    if check:
+        _check(s, "sbp_embedding_backward")
     return s
 
 

@@ -1,0 +1,508 @@
+// Rows of a table by id, scaled, and the table's gradient.
+//
+//   forward:   out[m] = scale * table[ids[m]] + add[m]                      (negative id: no row)
+//   backward:  dTable[v] = scale * sum of dOut[k] over the kept rows k with ids[k] = v
+//
+// The backward sums in a fixed order: the kept rows are sorted by id (a stable radix sort, so that rows of one id stay in
+// ascending order), the sorted list is cut into equal pieces, and a piece adds up the rows of each id in it.  An id whose rows
+// cross a piece's border leaves partial rows, which a last launch adds in the order of the pieces.  Nothing depends on how
+// often an id occurs: the most frequent one is spread over as many pieces as its rows fill.
+//
+// Bound by memory, in the main by clearing dTable where few of its rows get a gradient (50257 x 768: 154 MB).  The sort of
+// some ten thousand ids is a handful of short launches that leave the memory idle, so that blocks of those launches clear the
+// table, and the sums then write over the rows that have one.
+#include "row_copy.cuh"
+#include "row_math.cuh"
+
+namespace sbp {
+namespace {
+
+// ---- forward ----
+template <typename T, bool kAdd>
+__global__ void __launch_bounds__(kCopyThreads)
+embedding_forward_kernel(const uint4* __restrict__ table, const RowLength row, int64_t V, const int32_t* __restrict__ ids, int64_t M,
+                         float scale, const uint4* add, uint4* out, int32_t* status_word) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int64_t begin = (int64_t)blockIdx.x * kCopySpan, total = M * row.n;
+    const SpanRows span(begin, row);
+    int64_t src[kCopyUnroll];
+    uint4 v[kCopyUnroll], a[kCopyUnroll];
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+    for (int u = 0; u < kCopyUnroll; ++u) {
+        uint32_t q;
+        const int64_t c = span.place(threadIdx.x + u * kCopyThreads, row, &q);
+        src[u] = -1;
+        if (begin + threadIdx.x + u * kCopyThreads < total) {
+            const int64_t id = __ldg(ids + span.first + q);
+            if (id >= V) report_device_error(status_word, SBP_ERR_BAD_INDICES);
+            else if (id >= 0) src[u] = id * row.n + c;
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < kCopyUnroll; ++u) {
+        const int64_t i = begin + threadIdx.x + u * kCopyThreads;
+        v[u] = src[u] >= 0 ? __ldg(table + src[u]) : zero;
+        if constexpr (kAdd) a[u] = i < total ? ld_row(add + i) : zero;
+    }
+#pragma unroll
+    for (int u = 0; u < kCopyUnroll; ++u) {
+        const int64_t i = begin + threadIdx.x + u * kCopyThreads;
+        if (i >= total) continue;
+        constexpr int N = Vec<T>::N;
+        float f[N], g[N];
+        Vec<T>::unpack(v[u], f);
+        if constexpr (kAdd) Vec<T>::unpack(a[u], g);
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+            if constexpr (kAdd) f[e] = src[u] >= 0 ? fmaf(scale, f[e], g[e]) : g[e];
+            else f[e] = src[u] >= 0 ? scale * f[e] : 0.f;
+        }
+        out[i] = Vec<T>::pack(f);
+    }
+}
+
+// ---- backward: the sort ----
+constexpr int kSortThreads = 512, kSortItems = 8, kSortTile = kSortThreads * kSortItems, kSortWarps = kSortThreads / 32;
+constexpr int kDigits = 256, kSortMaxBlocks = 128;
+
+struct SortParams {
+    const int32_t *ids, *keep_rows, *M_keep_dev;
+    int64_t M, M_keep_cap, V;
+    int compact;                                      // dOut is packed: the source row is the place in the list
+    uint32_t* keys[2];
+    int32_t* rows[2];
+    uint32_t* hist;                                   // [blocks][kDigits]
+    int tiles;                                        // kSortTile pieces of a block
+    int blocks, passes, bits;                         // sorting blocks; digits of `bits` bits
+    uint4* clear;                                     // dTable, or nullptr
+    int64_t clear_vecs;
+    int32_t* status_word;
+};
+
+// The id of the m-th kept row (V: none), and where its gradient is.
+__device__ __forceinline__ uint32_t sort_input(const SortParams& p, int64_t m, int32_t* src) {
+    const int64_t row = mapped_row(p.keep_rows, m);
+    *src = p.compact ? (int32_t)m : (int32_t)row;
+    if (row < 0 || row >= p.M) return (uint32_t)p.V;
+    const int64_t id = __ldg(p.ids + row);
+    if (id >= p.V) report_device_error(p.status_word, SBP_ERR_BAD_INDICES);
+    return id >= 0 && id < p.V ? (uint32_t)id : (uint32_t)p.V;
+}
+
+// Blocks behind the sorting ones clear `part` of `parts` of dTable.
+__device__ __forceinline__ void clear_table(const SortParams& p, int part, int parts) {
+    if (p.clear == nullptr) return;
+    const int64_t lo = p.clear_vecs * part / parts, hi = p.clear_vecs * (part + 1) / parts;
+    const int64_t blocks = (int64_t)gridDim.x - p.blocks, stride = blocks * kSortThreads;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    int64_t i = lo + ((int64_t)blockIdx.x - p.blocks) * kSortThreads + threadIdx.x;
+    for (; i + 3 * stride < hi; i += 4 * stride) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) p.clear[i + u * stride] = zero;
+    }
+    for (; i < hi; i += stride) p.clear[i] = zero;
+}
+
+// Exclusive sums of one value a digit over the digits, by the first 256 threads; the others pass the barriers.
+__device__ __forceinline__ uint32_t digit_scan(uint32_t v, uint32_t* warp_sums) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    uint32_t s = v;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+        const uint32_t t = __shfl_up_sync(0xffffffffu, s, o);
+        if (lane >= o) s += t;
+    }
+    if (lane == 31 && warp < kDigits / 32) warp_sums[warp] = s;
+    __syncthreads();
+    uint32_t before = 0;
+    for (int w = 0; w < warp && w < kDigits / 32; ++w) before += warp_sums[w];
+    __syncthreads();
+    return before + s - v;
+}
+
+struct SortShared {
+    uint32_t base[kDigits];                           // where the next element of a digit goes
+    uint32_t count[kSortWarps][kDigits];
+    uint32_t warp_sums[kDigits / 32];
+};
+
+// Elements [begin, begin + kSortTile) of the list, below n: each goes to base[digit] plus the number of elements of its digit
+// before it; base moves on.  Warp w has the w-th 256 elements, 32 at a time, so the order of the list is kept.
+__device__ __forceinline__ void scatter_tile(const SortParams& p, SortShared& sh, int64_t begin, int64_t n, int pass) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&sh.count[0][0])[i] = 0u;
+    __syncthreads();
+    uint32_t key[kSortItems], rank[kSortItems];
+    int32_t row[kSortItems];
+    const int shift = pass * p.bits;
+    const uint32_t mask = (1u << p.bits) - 1u;
+    const int64_t first = begin + warp * (32 * kSortItems) + lane;
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+        const int64_t at = first + 32 * i;
+        key[i] = 0u;
+        row[i] = 0;
+        if (at < n) {
+            if (pass == 0) key[i] = sort_input(p, at, &row[i]);
+            else {
+                key[i] = p.keys[(pass + 1) & 1][at];
+                row[i] = p.rows[(pass + 1) & 1][at];
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+        const bool live = first + 32 * i < n;
+        const uint32_t d = key[i] >> shift & mask;
+        uint32_t peers = __ballot_sync(0xffffffffu, live);
+        for (int b = 0; b < p.bits; ++b) {
+            const uint32_t set = __ballot_sync(0xffffffffu, d >> b & 1u);
+            peers &= (d >> b & 1u) ? set : ~set;
+        }
+        const uint32_t before = live ? sh.count[warp][d] : 0u;
+        rank[i] = before + __popc(peers & ((1u << lane) - 1u));
+        __syncwarp();
+        if (live && (peers >> lane) == 1u) sh.count[warp][d] = before + __popc(peers);      // the last of them
+        __syncwarp();
+    }
+    __syncthreads();
+    if (threadIdx.x < kDigits) {                      // a warp's elements of a digit follow those of the warps before it
+        uint32_t at = sh.base[threadIdx.x];
+        for (int w = 0; w < kSortWarps; ++w) {
+            const uint32_t c = sh.count[w][threadIdx.x];
+            sh.count[w][threadIdx.x] = at;
+            at += c;
+        }
+        sh.base[threadIdx.x] = at;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kSortItems; ++i) {
+        if (first + 32 * i >= n) continue;
+        const uint32_t to = sh.count[warp][key[i] >> shift & mask] + rank[i];
+        p.keys[pass & 1][to] = key[i];
+        p.rows[pass & 1][to] = row[i];
+    }
+    __syncthreads();
+}
+
+// Counts of the digits of elements [begin, end), left in sh.base.
+__device__ __forceinline__ void count_digits(const SortParams& p, SortShared& sh, int64_t begin, int64_t end, int pass) {
+    if (threadIdx.x < kDigits) sh.base[threadIdx.x] = 0u;
+    __syncthreads();
+    const uint32_t mask = (1u << p.bits) - 1u;
+    for (int64_t at = begin + threadIdx.x; at < end; at += kSortThreads) {
+        int32_t src;
+        const uint32_t key = pass == 0 ? sort_input(p, at, &src) : p.keys[(pass + 1) & 1][at];
+        atomicAdd(&sh.base[key >> (pass * p.bits) & mask], 1u);
+    }
+    __syncthreads();
+}
+
+// The whole sort in one block.
+__global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(const SortParams p) {
+    __shared__ SortShared sh;
+    pdl_launch_dependents();
+    pdl_wait();
+    if (blockIdx.x >= (unsigned)p.blocks) return clear_table(p, 0, 1);
+    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap);
+    for (int pass = 0; pass < p.passes; ++pass) {
+        count_digits(p, sh, 0, n, pass);
+        const uint32_t start = digit_scan(threadIdx.x < kDigits ? sh.base[threadIdx.x] : 0u, sh.warp_sums);
+        if (threadIdx.x < kDigits) sh.base[threadIdx.x] = start;
+        __syncthreads();
+        scatter_tile(p, sh, 0, n, pass);
+    }
+}
+
+// One pass over more blocks: the digits of every block are counted, then every block adds up the counts in front of its own.
+__global__ void __launch_bounds__(kSortThreads) embedding_count_kernel(const SortParams p, int pass) {
+    __shared__ SortShared sh;
+    pdl_launch_dependents();
+    pdl_wait();
+    if (blockIdx.x >= (unsigned)p.blocks) return clear_table(p, 2 * pass, 2 * p.passes);
+    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap), span = (int64_t)p.tiles * kSortTile;
+    const int64_t begin = blockIdx.x * span, end = begin + span < n ? begin + span : n;
+    count_digits(p, sh, begin, end, pass);
+    if (threadIdx.x < kDigits) p.hist[blockIdx.x * kDigits + threadIdx.x] = sh.base[threadIdx.x];
+}
+__global__ void __launch_bounds__(kSortThreads) embedding_scatter_kernel(const SortParams p, int pass) {
+    __shared__ SortShared sh;
+    pdl_launch_dependents();
+    pdl_wait();
+    if (blockIdx.x >= (unsigned)p.blocks) return clear_table(p, 2 * pass + 1, 2 * p.passes);
+    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap), span = (int64_t)p.tiles * kSortTile;
+    const int64_t begin = blockIdx.x * span, end = begin + span < n ? begin + span : n;
+    if (begin >= end) return;
+    uint32_t all = 0u, before = 0u;
+    if (threadIdx.x < kDigits) {
+#pragma unroll 8
+        for (int b = 0; b < p.blocks; ++b) {
+            const uint32_t c = p.hist[b * kDigits + threadIdx.x];
+            all += c;
+            before += b < (int)blockIdx.x ? c : 0u;
+        }
+    }
+    const uint32_t start = digit_scan(all, sh.warp_sums);
+    if (threadIdx.x < kDigits) sh.base[threadIdx.x] = start + before;
+    __syncthreads();
+    for (int64_t at = begin; at < end; at += kSortTile) scatter_tile(p, sh, at, n, pass);
+}
+
+// ---- backward: the sums ----
+struct SumParams {
+    const uint4* dOut;
+    const uint32_t* keys;                             // sorted; V and above: no id
+    const int32_t* rows;
+    const int32_t* M_keep_dev;
+    int64_t M_keep_cap, V;
+    float *dTable, *partial;                          // partial [pieces][2][C]: the id that came in from the left, the one that goes on
+    int vecs, strips, piece, accumulate;              // 16-byte vectors of a row, 32-vector strips of it, places of a piece
+    float scale;
+};
+
+template <int N>
+__device__ __forceinline__ void put_sum(float* to, const float (&f)[N], float scale, bool add) {
+#pragma unroll
+    for (int e = 0; e < N; e += 4) {
+        float4* q = reinterpret_cast<float4*>(to + e);
+        float4 s = make_float4(scale * f[e], scale * f[e + 1], scale * f[e + 2], scale * f[e + 3]);
+        if (add) {
+            const float4 old = *q;
+            s.x += old.x;
+            s.y += old.y;
+            s.z += old.z;
+            s.w += old.w;
+        }
+        *q = s;
+    }
+}
+
+// A warp adds up one strip (32 vectors) of the rows of one piece.
+constexpr int kSumUnroll = 8;
+template <typename T>
+__global__ void __launch_bounds__(256) embedding_sum_kernel(const SumParams p) {
+    constexpr int N = Vec<T>::N;
+    pdl_launch_dependents();
+    pdl_wait();
+    const int lane = threadIdx.x & 31;
+    const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
+    const int64_t piece = warp / p.strips;
+    const int v = (int)(warp % p.strips) * 32 + lane;
+    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap);
+    const int64_t lo = piece * p.piece, hi = lo + p.piece < n ? lo + p.piece : n;
+    if (lo >= hi) return;
+    const uint32_t V = (uint32_t)p.V;
+    const bool in = v < p.vecs;
+    const int64_t C = (int64_t)p.vecs * N;
+    const uint32_t left = lo > 0 ? p.keys[lo - 1] : 0xffffffffu, right = hi < n ? p.keys[hi] : 0xffffffffu;
+    uint32_t cur = p.keys[lo];
+    float acc[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] = 0.f;
+    auto put = [&](bool last) {
+        if (!in) return;
+        if (cur == left) put_sum<N>(p.partial + piece * 2 * C + (int64_t)v * N, acc, 1.f, false);
+        else if (last && cur == right) put_sum<N>(p.partial + (piece * 2 + 1) * C + (int64_t)v * N, acc, 1.f, false);
+        else put_sum<N>(p.dTable + (int64_t)cur * C + (int64_t)v * N, acc, p.scale, p.accumulate != 0);
+    };
+    for (int64_t base = lo; base < hi && cur < V; base += 32) {
+        const uint32_t my_key = base + lane < hi ? p.keys[base + lane] : V;
+        const int32_t my_row = base + lane < hi ? p.rows[base + lane] : 0;
+        const int most = hi - base < 32 ? (int)(hi - base) : 32;
+        const int count = __popc(__ballot_sync(0xffffffffu, my_key < V && lane < most));       // (sorted: the ones with an id come first)
+        for (int j0 = 0; j0 < count; j0 += kSumUnroll) {
+            uint4 q[kSumUnroll];
+#pragma unroll
+            for (int u = 0; u < kSumUnroll; ++u) {
+                const int64_t r = __shfl_sync(0xffffffffu, my_row, (j0 + u) & 31);
+                q[u] = j0 + u < count && in ? ld_stream(p.dOut + r * p.vecs + v) : make_uint4(0u, 0u, 0u, 0u);
+            }
+#pragma unroll
+            for (int u = 0; u < kSumUnroll; ++u) {
+                const uint32_t k = __shfl_sync(0xffffffffu, my_key, (j0 + u) & 31);
+                if (j0 + u >= count) break;
+                if (k != cur) {
+                    put(false);
+                    cur = k;
+#pragma unroll
+                    for (int e = 0; e < N; ++e) acc[e] = 0.f;
+                }
+                float f[N];
+                Vec<T>::unpack(q[u], f);
+#pragma unroll
+                for (int e = 0; e < N; ++e) acc[e] += f[e];
+            }
+        }
+        if (count < most) {                           // the rest of the list has no ids
+            if (cur < V) put(false);
+            return;
+        }
+    }
+    if (cur < V) put(true);
+}
+
+// Adds the partial rows of the ids that cross a piece's border: the block of the piece in which such an id begins.  Eight warps
+// take the pieces in turns, and their sums are added in the order of the warps.
+template <typename T>
+__global__ void __launch_bounds__(256) embedding_join_kernel(const SumParams p) {
+    constexpr int N = Vec<T>::N;
+    __shared__ float part[8][32][N + 1];
+    pdl_launch_dependents();
+    pdl_wait();
+    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap);
+    const int64_t piece = blockIdx.x / p.strips, lo = piece * p.piece, hi = lo + p.piece;
+    if (hi >= n) return;
+    const uint32_t k = p.keys[hi - 1];
+    if (k >= (uint32_t)p.V || p.keys[hi] != k || (lo > 0 && p.keys[lo - 1] == k)) return;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t pieces = (n + p.piece - 1) / p.piece;
+    int64_t end = piece + 2, top = pieces;            // pieces [piece + 1, end) begin with this id
+    while (end < top) {
+        const int64_t mid = (end + top) / 2;
+        if (p.keys[mid * p.piece] == k) end = mid + 1;
+        else top = mid;
+    }
+    const int v = (int)(blockIdx.x % p.strips) * 32 + lane;
+    const int64_t C = (int64_t)p.vecs * N;
+    float acc[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) acc[e] = 0.f;
+    if (v < p.vecs) {
+#pragma unroll 4
+        for (int64_t q = piece + warp; q < end; q += 8) {
+            float f[N];
+            load_f32<N>(p.partial + (q * 2 + (q == piece ? 1 : 0)) * C + (int64_t)v * N, f);
+#pragma unroll
+            for (int e = 0; e < N; ++e) acc[e] += f[e];
+        }
+    }
+#pragma unroll
+    for (int e = 0; e < N; ++e) part[warp][lane][e] = acc[e];
+    __syncthreads();
+    if (warp != 0 || v >= p.vecs) return;
+#pragma unroll
+    for (int w = 1; w < 8; ++w)
+#pragma unroll
+        for (int e = 0; e < N; ++e) acc[e] += part[w][lane][e];
+    put_sum<N>(p.dTable + (int64_t)k * C + (int64_t)v * N, acc, p.scale, p.accumulate != 0);
+}
+
+// ---- host ----
+struct SumShape {
+    int strips, piece;
+    int64_t pieces;
+};
+// pieces: enough warps for the device (32 an SM), and eight places at least, so that a piece's own loads overlap
+inline SumShape sum_shape(sbp_dtype dt, int64_t M_keep_cap, int64_t C) {
+    SumShape s;
+    const int64_t vecs = C / (dt == SBP_BF16 ? 8 : 4);
+    s.strips = (int)((vecs + 31) / 32);
+    const int64_t want = (int64_t)kNumSMs * 32 / s.strips, p = (M_keep_cap + want) / (want > 0 ? want : 1);
+    s.piece = (int)(p < 8 ? 8 : p);
+    s.pieces = (M_keep_cap + s.piece - 1) / s.piece;
+    return s;
+}
+struct SortShape {
+    int blocks, tiles, passes, bits;
+};
+inline SortShape sort_shape(int64_t M_keep_cap, int64_t V) {
+    SortShape s;
+    int bits = 1;
+    while ((V >> bits) != 0) ++bits;                  // keys 0 .. V
+    s.passes = (bits + 7) / 8;
+    s.bits = (bits + s.passes - 1) / s.passes;
+    const int64_t tiles = (M_keep_cap + kSortTile - 1) / kSortTile;
+    s.tiles = (int)((tiles + kSortMaxBlocks - 1) / kSortMaxBlocks);
+    if (s.tiles < 1) s.tiles = 1;
+    s.blocks = (int)((tiles + s.tiles - 1) / s.tiles);
+    return s;
+}
+inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
+
+}  // namespace
+
+cudaError_t launch_embedding_forward(sbp_dtype dt, const void* table, int64_t V, int64_t C, const int32_t* ids, int64_t M, float scale,
+                                     const void* add, void* out, int32_t* status_word, cudaStream_t stream) {
+    const int64_t vecs = C / (dt == SBP_BF16 ? 8 : 4);
+    const RowLength row(vecs);
+    const dim3 grid((unsigned)copy_blocks(M * vecs)), block(kCopyThreads);
+    auto go = [&](auto kernel) {
+        return launch_pdl(kernel, grid, block, 0, stream, (const uint4*)table, row, V, ids, M, scale, (const uint4*)add, (uint4*)out, status_word);
+    };
+    if (dt == SBP_BF16) return add ? go(embedding_forward_kernel<__nv_bfloat16, true>) : go(embedding_forward_kernel<__nv_bfloat16, false>);
+    return add ? go(embedding_forward_kernel<float, true>) : go(embedding_forward_kernel<float, false>);
+}
+
+size_t embedding_backward_workspace_bytes(sbp_dtype dt, int64_t M_keep_cap, int64_t C) {
+    const SumShape s = sum_shape(dt, M_keep_cap, C);
+    return 4 * up256((size_t)M_keep_cap * 4) + up256((size_t)kSortMaxBlocks * kDigits * 4) + up256((size_t)s.pieces * 2 * (size_t)C * 4);
+}
+
+cudaError_t launch_embedding_backward(sbp_dtype dt, const void* dOut, bool compact, const int32_t* ids, const int32_t* keep_rows,
+                                      const int32_t* M_keep_dev, int64_t M, int64_t M_keep_cap, int64_t V, int64_t C, float scale,
+                                      float* dTable, bool accumulate, void* workspace, int32_t* status_word, cudaStream_t stream) {
+    const SortShape so = sort_shape(M_keep_cap, V);
+    const SumShape su = sum_shape(dt, M_keep_cap, C);
+    uint8_t* ws = static_cast<uint8_t*>(workspace);
+    const size_t list = up256((size_t)M_keep_cap * 4);
+    SortParams p = {};
+    p.ids = ids;
+    p.keep_rows = keep_rows;
+    p.M_keep_dev = M_keep_dev;
+    p.M = M;
+    p.M_keep_cap = M_keep_cap;
+    p.V = V;
+    p.compact = compact;
+    p.keys[0] = (uint32_t*)ws;
+    p.keys[1] = (uint32_t*)(ws + list);
+    p.rows[0] = (int32_t*)(ws + 2 * list);
+    p.rows[1] = (int32_t*)(ws + 3 * list);
+    p.hist = (uint32_t*)(ws + 4 * list);
+    p.tiles = so.tiles;
+    p.blocks = so.blocks;
+    p.passes = so.passes;
+    p.bits = so.bits;
+    p.clear = accumulate ? nullptr : (uint4*)dTable;
+    p.clear_vecs = V * (C / 4);
+    p.status_word = status_word;
+    const int64_t want = (p.clear_vecs + 4 * kSortThreads - 1) / (4 * kSortThreads);
+    const int clear_blocks = accumulate ? 0 : (int)(want < 2 * kNumSMs ? want : 2 * kNumSMs);
+    const dim3 grid((unsigned)(so.blocks + clear_blocks)), block(kSortThreads);
+    if (grid.x == 0) return cudaSuccess;              // no rows, and nothing to clear
+    cudaError_t e;
+    if (so.blocks <= 1) {
+        if ((e = launch_pdl(embedding_sort_kernel, grid, block, 0, stream, p)) != cudaSuccess) return e;
+    } else {
+        for (int pass = 0; pass < so.passes; ++pass) {
+            if ((e = launch_pdl(embedding_count_kernel, grid, block, 0, stream, p, pass)) != cudaSuccess) return e;
+            if ((e = launch_pdl(embedding_scatter_kernel, grid, block, 0, stream, p, pass)) != cudaSuccess) return e;
+        }
+    }
+    if (M_keep_cap == 0) return cudaSuccess;
+    SumParams s = {};
+    s.dOut = (const uint4*)dOut;
+    s.keys = p.keys[(so.passes - 1) & 1];
+    s.rows = p.rows[(so.passes - 1) & 1];
+    s.M_keep_dev = M_keep_dev;
+    s.M_keep_cap = M_keep_cap;
+    s.V = V;
+    s.dTable = dTable;
+    s.partial = (float*)(ws + 4 * list + up256((size_t)kSortMaxBlocks * kDigits * 4));
+    s.vecs = (int)(C / (dt == SBP_BF16 ? 8 : 4));
+    s.strips = su.strips;
+    s.piece = su.piece;
+    s.accumulate = accumulate;
+    s.scale = scale;
+    const int64_t warps = su.pieces * su.strips;
+    const dim3 sum_grid((unsigned)((warps + 7) / 8)), join_grid((unsigned)warps);
+    e = dt == SBP_BF16 ? launch_pdl(embedding_sum_kernel<__nv_bfloat16>, sum_grid, dim3(256), 0, stream, s)
+                       : launch_pdl(embedding_sum_kernel<float>, sum_grid, dim3(256), 0, stream, s);
+    if (e != cudaSuccess || su.pieces < 2) return e;
+    return dt == SBP_BF16 ? launch_pdl(embedding_join_kernel<__nv_bfloat16>, join_grid, dim3(256), 0, stream, s)
+                          : launch_pdl(embedding_join_kernel<float>, join_grid, dim3(256), 0, stream, s);
+}
+
+}  // namespace sbp

@@ -441,6 +441,50 @@ sbp_status sbp_block_norm_backward(sbp_dtype dt, sbp_norm norm, const void* dR, 
 }
 
 namespace {
+// shared argument checks of the two embedding calls
+sbp_status embedding_arguments(sbp_dtype dt, int64_t M, int64_t V, int64_t C, double scale, const int32_t* ids) {
+    if (dt != SBP_F32 && dt != SBP_BF16) return SBP_ERR_INVALID_ARG;
+    if (M <= 0 || M >= (1ll << 31) || V <= 0 || V >= (1ll << 31) || C <= 0 || C >= (1ll << 24)) return SBP_ERR_INVALID_ARG;
+    if (!isfinite(scale) || !isfinite((float)scale)) return SBP_ERR_INVALID_ARG;
+    if (ids == nullptr || (reinterpret_cast<uintptr_t>(ids) & 3u)) return SBP_ERR_INVALID_ARG;
+    return (C * (dt == SBP_BF16 ? 2 : 4)) % 16 != 0 ? SBP_ERR_UNSUPPORTED : SBP_OK;
+}
+}  // namespace
+
+sbp_status sbp_embedding_forward(sbp_dtype dt, const void* table, int64_t V, int64_t C, const int32_t* ids, int64_t M, double scale,
+                                 const void* add, void* out, int32_t* status_word, void* stream) {
+    const sbp_status s = embedding_arguments(dt, M, V, C, scale, ids);
+    if (s == SBP_ERR_INVALID_ARG) return s;
+    if (table == nullptr || out == nullptr || !aligned16(table) || !aligned16(add) || !aligned16(out)) return SBP_ERR_INVALID_ARG;
+    if (s != SBP_OK) return s;
+    const cudaError_t e = launch_embedding_forward(dt, table, V, C, ids, M, (float)scale, add, out, status_word, (cudaStream_t)stream);
+    return e == cudaSuccess ? SBP_OK : SBP_ERR_CUDA;
+}
+
+size_t sbp_embedding_backward_workspace_bytes(sbp_dtype dt, int64_t M_keep_cap, int64_t V, int64_t C) {
+    if ((dt != SBP_F32 && dt != SBP_BF16) || M_keep_cap <= 0 || M_keep_cap >= (1ll << 31) || V <= 0 || C <= 0 || C >= (1ll << 24)) return 256;
+    return align_up(embedding_backward_workspace_bytes(dt, M_keep_cap, C), 256);
+}
+
+sbp_status sbp_embedding_backward(sbp_dtype dt, const void* dOut, const int32_t* ids, const int32_t* keep_rows, const int32_t* M_keep_dev,
+                                  int64_t M, int64_t M_keep_cap, int64_t V, int64_t C, double scale, float* dTable, uint32_t flags,
+                                  void* workspace, size_t workspace_bytes, int32_t* status_word, void* stream) {
+    const sbp_status s = embedding_arguments(dt, M, V, C, scale, ids);
+    if (s == SBP_ERR_INVALID_ARG) return s;
+    if (dOut == nullptr || dTable == nullptr || !aligned16(dOut) || !aligned16(dTable)) return SBP_ERR_INVALID_ARG;
+    if (M_keep_cap < 0 || M_keep_cap > M) return SBP_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(keep_rows) & 3u) || (reinterpret_cast<uintptr_t>(M_keep_dev) & 3u)) return SBP_ERR_INVALID_ARG;
+    if (s != SBP_OK) return s;
+    if (M_keep_cap > 0 && (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
+                           workspace_bytes < sbp_embedding_backward_workspace_bytes(dt, M_keep_cap, V, C)))
+        return SBP_ERR_WORKSPACE;
+    const cudaError_t e = launch_embedding_backward(dt, dOut, (flags & SBP_FLAG_DY_COMPACT) != 0, ids, keep_rows, M_keep_dev, M, M_keep_cap, V, C,
+                                                    (float)scale, dTable, (flags & SBP_FLAG_ACCUMULATE) != 0, workspace, status_word,
+                                                    (cudaStream_t)stream);
+    return e == cudaSuccess ? SBP_OK : SBP_ERR_CUDA;
+}
+
+namespace {
 // shared argument checks of the two patch calls; returns SBP_OK and the output grid when the geometry is usable
 sbp_status patch_geometry(sbp_dtype dt, int64_t B, int64_t H, int64_t W, int64_t C, int64_t k, int64_t stride, int64_t M_keep_cap,
                           int64_t* Ho, int64_t* Wo) {

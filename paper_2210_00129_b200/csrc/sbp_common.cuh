@@ -221,6 +221,14 @@ cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR,
                                        float* dpre_w, float* dpre_b, bool accumulate, float* workspace, const int32_t* status_word,
                                        cudaStream_t stream);
 
+// rows of a table by id, and the table's gradient (embedding.cu)
+cudaError_t launch_embedding_forward(sbp_dtype dt, const void* table, int64_t V, int64_t C, const int32_t* ids, int64_t M, float scale,
+                                     const void* add, void* out, int32_t* status_word, cudaStream_t stream);
+size_t embedding_backward_workspace_bytes(sbp_dtype dt, int64_t M_keep_cap, int64_t C);
+cudaError_t launch_embedding_backward(sbp_dtype dt, const void* dOut, bool compact, const int32_t* ids, const int32_t* keep_rows,
+                                      const int32_t* M_keep_dev, int64_t M, int64_t M_keep_cap, int64_t V, int64_t C, float scale,
+                                      float* dTable, bool accumulate, void* workspace, int32_t* status_word, cudaStream_t stream);
+
 // stride >= kernel convolutions as linear layers on patch rows: gather of the kept patches, scatter of their gradients
 cudaError_t launch_patch_gather(const void* X, int64_t H, int64_t W, int64_t pos_bytes, int64_t k, int64_t s,
                                 const int32_t* keep_rows, const int32_t* M_keep_dev, int64_t M_keep_cap, void* X_keep,
