@@ -17,6 +17,7 @@
  *   sbp_patch_cache / sbp_patch_scatter  stride >= kernel convolutions as linear layers on patch rows (Sec. 3.2.2)
  *   sbp_block_norm_forward / _backward  norms before and after a block with its gate and residual scale
  *   sbp_embedding_forward / _backward   rows of a table by id; the table's gradient from the kept rows
+ *   sbp_orthogonalize    the update of a weight from its gradient: momentum and Newton-Schulz orthogonalisation
  *
  * Nothing is rescaled by 1/r: Eq. 1 keeps the plain 1/B factor.
  *
@@ -78,7 +79,8 @@ enum {
     SBP_FLAG_DX_COMPACT = 32, /* dX receives only the kept rows, packed: [M_keep_cap, C_in]; no zero rows are written */
     SBP_FLAG_W_OUT_IN = 64,   /* W, and dW, are stored [C_out, C_in] (the usual layout of framework linear layers) */
     SBP_FLAG_ATTN_ALL_KEYS = 128, /* sbp_attention_backward: keys and values are all tokens, only queries are dropped */
-    SBP_FLAG_ATTN_KEPT_ROWS_ONLY = 256 /* sbp_attention_backward: write only the rows in the token lists, leave every other row alone */
+    SBP_FLAG_ATTN_KEPT_ROWS_ONLY = 256, /* sbp_attention_backward: write only the rows in the token lists, leave every other row alone */
+    SBP_FLAG_NESTEROV = 512   /* sbp_orthogonalize: look one step ahead along the averaged gradient */
 };
 
 const char* sbp_status_string(sbp_status s);
@@ -365,6 +367,36 @@ sbp_status sbp_embedding_backward(sbp_dtype dt, const void* dOut /* dev */, cons
                                   int64_t M, int64_t M_keep_cap, int64_t V, int64_t C, double scale, float* dTable /* dev */,
                                   uint32_t flags, void* workspace /* dev */, size_t workspace_bytes,
                                   int32_t* status_word /* dev, nullable */, void* stream);
+
+/* Scratch bytes sbp_orthogonalize needs for these sizes (never 0). */
+size_t sbp_orthogonalize_workspace_bytes(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols);
+
+/*
+ * The update that a weight's gradient becomes: momentum, then orthogonalisation by Newton-Schulz products (as the Muon
+ * optimiser does), for `count` matrices of one shape - the dW of one layer shape over all blocks, as sbp_linear_backward
+ * writes them, in either weight layout.  Per matrix:
+ *   momentum given:  momentum <- beta * momentum + G,  U = momentum, or G + beta * momentum with SBP_FLAG_NESTEROV
+ *   momentum NULL:   U = G
+ *   X = U / (|U| + eps)            (Frobenius norm)
+ *   steps times:  X <- a X + (b A + c A^2) X  with A = X X^T,  (a, b, c) = (3.4445, -4.7750, 2.0315)
+ *                 (rows > cols: X <- a X + X (b A + c A^2) with A = X^T X)
+ *   O = scale * X
+ * G, momentum fp32 [count, rows, cols]; O [count, rows, cols] in dt.  Any rows and cols from 1 to 65536; count up to 65535.
+ * The caller applies O to its weights (and passes what its recipe scales by, e.g. sqrt(max(1, rows / cols))).
+ * Precision: the norm in 64 bits; X as two fp16 numbers (22 bits) wherever it carries a direction on, products on the
+ * tensor cores with fp32 sums.  SBP_BF16: operands of the products in fp16, but for the diagonals of A and of its
+ * polynomial (fp32) - about 1e-3 of the result's norm, against 1.7e-3 that the rounding of O to bf16 brings; sides up to
+ * 128, and SBP_F32: both fp16 numbers in the products (three instead of one), about 1e-6 of the norm.  What is smaller than
+ * 2^-23 of the largest numbers of U may show, grown by a factor of up to a ^ steps, in directions where U has none.
+ * A matrix of zeros gives zeros (with eps = 0: NaN); infinite and NaN gradients give NaN in their matrix.
+ * SBP_ERR_INVALID_ARG for null or misaligned (16 bytes) pointers, sizes below 1, steps outside 1 .. 32, beta, eps or scale not
+ * finite, eps < 0, SBP_FLAG_NESTEROV without momentum; SBP_ERR_UNSUPPORTED for larger sizes; SBP_ERR_WORKSPACE as for
+ * sbp_linear_backward.  No buffer overlaps another.  status_word as for sbp_linear_backward.  Deterministic.
+ */
+sbp_status sbp_orthogonalize(sbp_dtype dt, const float* G /* dev */, float* momentum /* dev, nullable */, double beta, int64_t count,
+                             int64_t rows, int64_t cols, int steps, double eps, double scale, void* O /* dev */, uint32_t flags,
+                             void* workspace /* dev */, size_t workspace_bytes, int32_t* status_word /* dev, nullable */,
+                             void* stream);
 
 /*
  * Convolutions with stride >= kernel size as SBP layers (Sec. 3.2.2, the text after Eq. 6: with s >= k the

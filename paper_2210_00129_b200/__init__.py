@@ -30,13 +30,14 @@ SBP_NORM_LAYER, SBP_NORM_RMS = 0, 1
 SBP_MASK_RANDOM, SBP_MASK_GRID, SBP_MASK_TEMPORAL, SBP_MASK_TEMPORAL_GRID = 0, 1, 2, 3
 SBP_FLAG_SHARE_MASK, SBP_FLAG_ACCUMULATE, SBP_FLAG_VALIDATE, SBP_FLAG_PLAIN_FMA = 1, 2, 4, 8
 SBP_FLAG_DY_COMPACT, SBP_FLAG_DX_COMPACT, SBP_FLAG_W_OUT_IN, SBP_FLAG_ATTN_ALL_KEYS = 16, 32, 64, 128
-SBP_FLAG_ATTN_KEPT_ROWS_ONLY = 256
+SBP_FLAG_ATTN_KEPT_ROWS_ONLY, SBP_FLAG_NESTEROV = 256, 512
 
 EXPORTS = ("sbp_status_string", "sbp_keep_count", "sbp_sample_keep", "sbp_forward_cache", "sbp_linear_forward",
            "sbp_linear_backward_workspace_bytes", "sbp_linear_backward", "sbp_linear_backward_kernel_count",
            "sbp_plan_search_count", "sbp_act_backward", "sbp_block_norm_forward",
            "sbp_block_norm_backward_workspace_bytes", "sbp_block_norm_backward", "sbp_embedding_forward",
-           "sbp_embedding_backward_workspace_bytes", "sbp_embedding_backward", "sbp_attention_backward", "sbp_patch_cache", "sbp_patch_scatter_workspace_bytes",
+           "sbp_embedding_backward_workspace_bytes", "sbp_embedding_backward", "sbp_orthogonalize_workspace_bytes",
+           "sbp_orthogonalize", "sbp_attention_backward", "sbp_patch_cache", "sbp_patch_scatter_workspace_bytes",
            "sbp_patch_scatter", "sbp_step_host_arena_bytes", "sbp_step_host", "sbp_bias_grad_static",
            "sbp_selftest_bounded_wait", "sbp_probe_gather_ring", "sbp_probe_mma_rate", "sbp_probe_mma_pair_rate", "sbp_probe_operand_feed")
 
@@ -112,6 +113,10 @@ def load_library() -> ctypes.CDLL:
     lib.sbp_embedding_backward_workspace_bytes.restype = sz
     lib.sbp_embedding_backward.argtypes = [ci, vp, vp, vp, vp, i64, i64, i64, i64, dbl, vp, u32, vp, sz, vp, vp]
     lib.sbp_embedding_backward.restype = ci
+    lib.sbp_orthogonalize_workspace_bytes.argtypes = [ci, i64, i64, i64]
+    lib.sbp_orthogonalize_workspace_bytes.restype = sz
+    lib.sbp_orthogonalize.argtypes = [ci, vp, vp, dbl, i64, i64, i64, ci, dbl, dbl, vp, u32, vp, sz, vp, vp]
+    lib.sbp_orthogonalize.restype = ci
     lib.sbp_plan_search_count.argtypes = []
     lib.sbp_plan_search_count.restype = i64
     lib.sbp_step_host_arena_bytes.argtypes = [ci, ci, i64, i64, i64, i64, i64, dbl]
@@ -332,6 +337,20 @@ def sbp_embedding_backward(dt, dOut, ids, keep_rows, M_keep_dev, M, M_keep_cap, 
                                         workspace_bytes, status_word, _stream(stream))
     if check:
         _check(s, "sbp_embedding_backward")
+    return s
+
+
+def sbp_orthogonalize_workspace_bytes(dt, count, rows, cols) -> int:
+    return int(load_library().sbp_orthogonalize_workspace_bytes(dt, count, rows, cols))
+
+
+def sbp_orthogonalize(dt, G, momentum, beta, count, rows, cols, steps, eps, scale, O, flags, workspace, workspace_bytes,
+                      status_word=None, stream=None, check=True) -> int:
+    """Momentum and Newton-Schulz orthogonalisation of `count` weight gradients [rows, cols] (fp32) into O (dt)."""
+    s = _calls().sbp_orthogonalize(dt, G, momentum, beta, count, rows, cols, steps, eps, scale, O, flags, workspace, workspace_bytes,
+                                   status_word, _stream(stream))
+    if check:
+        _check(s, "sbp_orthogonalize")
     return s
 
 

@@ -104,6 +104,7 @@ PyMethodDef g_methods[] = {
     SBP_CALL(sbp_block_norm_backward),
     SBP_CALL(sbp_embedding_forward),
     SBP_CALL(sbp_embedding_backward),
+    SBP_CALL(sbp_orthogonalize),
     SBP_CALL(sbp_patch_cache),
     SBP_CALL(sbp_patch_scatter),
     SBP_CALL(sbp_step_host),

@@ -484,6 +484,28 @@ sbp_status sbp_embedding_backward(sbp_dtype dt, const void* dOut, const int32_t*
     return e == cudaSuccess ? SBP_OK : SBP_ERR_CUDA;
 }
 
+size_t sbp_orthogonalize_workspace_bytes(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols) {
+    if ((dt != SBP_F32 && dt != SBP_BF16) || count <= 0 || rows <= 0 || cols <= 0 || !orthogonalize_supported(count, rows, cols)) return 256;
+    return align_up(orthogonalize_workspace_bytes(dt, count, rows, cols), 256);
+}
+
+sbp_status sbp_orthogonalize(sbp_dtype dt, const float* G, float* momentum, double beta, int64_t count, int64_t rows, int64_t cols, int steps,
+                             double eps, double scale, void* O, uint32_t flags, void* workspace, size_t workspace_bytes, int32_t* status_word,
+                             void* stream) {
+    if (dt != SBP_F32 && dt != SBP_BF16) return SBP_ERR_INVALID_ARG;
+    if (G == nullptr || O == nullptr || !aligned16(G) || !aligned16(momentum) || !aligned16(O)) return SBP_ERR_INVALID_ARG;
+    if (count <= 0 || rows <= 0 || cols <= 0 || steps < 1 || steps > 32) return SBP_ERR_INVALID_ARG;
+    if (!isfinite((float)beta) || !isfinite((float)scale) || !isfinite(eps) || eps < 0.0) return SBP_ERR_INVALID_ARG;
+    if ((flags & SBP_FLAG_NESTEROV) && momentum == nullptr) return SBP_ERR_INVALID_ARG;
+    if (!orthogonalize_supported(count, rows, cols)) return SBP_ERR_UNSUPPORTED;
+    if (workspace == nullptr || (reinterpret_cast<uintptr_t>(workspace) & 255u) ||
+        workspace_bytes < sbp_orthogonalize_workspace_bytes(dt, count, rows, cols))
+        return SBP_ERR_WORKSPACE;
+    const cudaError_t e = launch_orthogonalize(dt, G, momentum, (float)beta, (flags & SBP_FLAG_NESTEROV) != 0, count, rows, cols, steps, eps,
+                                               (float)scale, O, workspace, status_word, (cudaStream_t)stream);
+    return e == cudaSuccess ? SBP_OK : SBP_ERR_CUDA;
+}
+
 namespace {
 // shared argument checks of the two patch calls; returns SBP_OK and the output grid when the geometry is usable
 sbp_status patch_geometry(sbp_dtype dt, int64_t B, int64_t H, int64_t W, int64_t C, int64_t k, int64_t stride, int64_t M_keep_cap,

@@ -229,6 +229,12 @@ cudaError_t launch_embedding_backward(sbp_dtype dt, const void* dOut, bool compa
                                       const int32_t* M_keep_dev, int64_t M, int64_t M_keep_cap, int64_t V, int64_t C, float scale,
                                       float* dTable, bool accumulate, void* workspace, int32_t* status_word, cudaStream_t stream);
 
+// Newton-Schulz orthogonalisation of updates (orthogonalize.cu)
+bool   orthogonalize_supported(int64_t count, int64_t rows, int64_t cols);
+size_t orthogonalize_workspace_bytes(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols);
+cudaError_t launch_orthogonalize(sbp_dtype dt, const float* G, float* momentum, float beta, bool nesterov, int64_t count, int64_t rows, int64_t cols,
+                                 int steps, double eps, float scale, void* O, void* workspace, int32_t* status_word, cudaStream_t stream);
+
 // stride >= kernel convolutions as linear layers on patch rows: gather of the kept patches, scatter of their gradients
 cudaError_t launch_patch_gather(const void* X, int64_t H, int64_t W, int64_t pos_bytes, int64_t k, int64_t s,
                                 const int32_t* keep_rows, const int32_t* M_keep_dev, int64_t M_keep_cap, void* X_keep,

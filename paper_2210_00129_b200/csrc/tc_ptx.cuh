@@ -83,6 +83,13 @@ __device__ __forceinline__ void tma_load_2d_warp(uint32_t dst, const CUtensorMap
         "@q cp.async.bulk.tensor.2d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];\n\t}"
         ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(bar), "r"((uint32_t)leader) : "memory");
 }
+// a box of a 3-D tensor, as above
+__device__ __forceinline__ void tma_load_3d_warp(uint32_t dst, const CUtensorMap* map, int x, int y, int z, uint32_t bar, bool leader) {
+    asm volatile(
+        "{\n\t.reg .pred q;\n\tsetp.ne.b32 q, %6, 0;\n\t"
+        "@q cp.async.bulk.tensor.3d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4}], [%5];\n\t}"
+        ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(x), "r"(y), "r"(z), "r"(bar), "r"((uint32_t)leader) : "memory");
+}
 // ---- TMA stores (shared -> global, bulk async-group completion) ----
 // 3-D box at element coordinates (x, y, z); x * element size must be a multiple of 16 bytes
 __device__ __forceinline__ void tma_store_3d(const CUtensorMap* map, uint32_t src, int x, int y, int z) {
@@ -178,7 +185,11 @@ __host__ __device__ constexpr uint32_t umma_idesc_bf16(int M, int N, bool a_mn_m
     return (1u << 4) | (1u << 7) | (1u << 10) | ((a_mn_major ? 1u : 0u) << 15) | ((b_mn_major ? 1u : 0u) << 16) |
            ((uint32_t)(N >> 3) << 17) | ((uint32_t)(M >> 4) << 24);
 }
-// The same descriptor split for stepping: the high word is the same for every operand here (1024 bytes between eight-row
+// the same with fp16 operands (type 0)
+__host__ __device__ constexpr uint32_t umma_idesc_f16(int M, int N, bool a_mn_major, bool b_mn_major) {
+    return umma_idesc_bf16(M, N, a_mn_major, b_mn_major) & ~((1u << 7) | (1u << 10));
+}
+// The operand descriptor split for stepping: the high word is the same for every operand here (1024 bytes between eight-row
 // groups), the low word holds the start address and the leading-dimension offset, both in 16-byte units, so that stepping
 // through an operand is one 32-bit addition.
 __device__ __forceinline__ uint32_t umma_desc_lo(uint32_t saddr, uint32_t lbo_bytes) {
