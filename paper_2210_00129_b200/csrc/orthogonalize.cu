@@ -16,9 +16,13 @@
 // it for each 64 deep block), is read out every kPartBlocks blocks and added up in fp32 registers, the small products first.
 // X, A and B are held times 2^12, which keeps the small numbers of large matrices out of fp16's subnormals.
 //
-// Each product is one launch of a persistent kernel over 128 x 128 tiles of all matrices: TMA loads (either orientation of X
-// is read in place), tcgen05.mma into two accumulators in turns, and an epilogue that forms the next operand from the sums.
-// A and B are symmetric: only tiles on and above the diagonal are made, and stored both ways.
+// All products of a call run in one launch of a persistent kernel.  Its items are the tiles of all products of all matrices, in the
+// order step, product, matrix, tile; blocks draw the next one from a counter, and an item waits until the tiles of its matrix
+// that it depends on are done (a count for each matrix).  Items only wait for items drawn before them, so some block can always
+// go on, however many are resident; with several matrices nothing waits, and the epilogue of one tile runs under the products of
+// the next.  (One launch a product, seventeen a call, cost 8 us each before their first tile.)  Operands come by TMA, X in either
+// orientation as it lies; tcgen05.mma into accumulators in turns; the epilogue forms the next operand from the sums.  A and B
+// are symmetric: only tiles on and above the diagonal are made, and stored both ways.
 #include "tc_ptx.cuh"
 
 #include <cuda_fp16.h>
@@ -31,61 +35,130 @@ constexpr float kUp = 4096.f, kDown = 1.f / 4096.f;                 // X, A and 
 constexpr int kExactSide = 128;
 constexpr int kPartBlocks = 4;
 
-constexpr int kTile = 128, kDeep = 64, kUmmaDeep = 16;
+constexpr int kTile = 128, kDeep = 64, kUmmaDeep = 16;               // rows of a tile, depth of a stage and of an instruction
 constexpr uint32_t kRow = 128;                                      // bytes of a 64 deep row
 constexpr uint32_t kOperand = kTile * kRow, kHalfOperand = 64 * kRow;
-constexpr int kStages = 4;
-constexpr uint32_t kStage = 2 * kOperand;
-constexpr uint32_t kStagingBytes = 32 * 64 * 4;                     // of an epilogue warp: 32 rows x 64 sums
-constexpr uint32_t kMirrorBytes = 64 * 32 * 2;                      // the same tile the other way, fp16, twice
-constexpr uint32_t kWarpBytes = kStagingBytes + 2 * kMirrorBytes;
-constexpr uint32_t kOrthoSmem = kStages * kStage + 256 + 4 * kWarpBytes + 1024;
-constexpr int kOrthoThreads = 192;                                  // 0-3 epilogue, 4 copies, 5 products
-constexpr int kEpilogueBarrier = 1;
+constexpr int kCopyWarp = 0, kProductWarp = 1, kTellWarp = 2, kDrawWarp = 3, kFirstEpilogueWarp = 4;
+constexpr uint32_t kStagingBytes = 32 * 1024;                       // of all epilogue warps
+constexpr uint32_t kHalfBytes = 32 * 32 * 2;                        // 32 x 32 numbers in fp16
+constexpr uint32_t kRing = 192 * 1024, kControl = 512;
+constexpr uint32_t kOrthoSmem = kRing + kControl + kStagingBytes + 1024;
+constexpr int kMostStages = 6, kItems = 4;
 
 enum { kGram = 0, kPoly = 1, kStep = 2 };
 
 struct OrthoControl {
-    uint64_t full[kStages], empty[kStages], acc_full[2], acc_empty[2];
+    uint64_t full[kMostStages], empty[kMostStages];                  // a stage's operands: in place, read
+    uint64_t acc_full[2], acc_empty[2], small_full[2], small_empty[2];
+    uint64_t item_full[kItems], item_empty[kItems], stored[kItems];  // an item: drawn and ready, read by all, its tile written
+    uint32_t item[kItems];
     uint32_t tmem_slot;
     int abort_flag;
 };
-static_assert(sizeof(OrthoControl) <= 256, "control block");
+static_assert(sizeof(OrthoControl) <= kControl, "control block");
 
 struct OrthoParams {
-    __half *X, *S;                   // planes [2 buffers][first, second][count][rows][ldx] and [A, B][first(, second)][count][m][ldm]
+    __half *X, *S;                   // planes [2 buffers][first, second][count][rows][ldx] and [A(, its second), B, its second][count][m][ldm]
     float *diag_a, *diag_b;          // [count][ldm]
-    void* out;                       // the last step's result [count][rows][cols], else nullptr
+    void* out;                       // the last step's result [count][rows][cols]
+    uint32_t* drawn;                 // items drawn so far
+    int32_t* done;                   // [count]: finished tiles of the matrix
     int64_t x_plane, s_plane;        // elements of one matrix's plane
-    int count, rows, cols, m, ldx, ldm;
-    int buffer;                      // of X, read; the other one is written
-    int s_planes;                    // 1, or 2 where A and B have their second numbers
-    int tiles_i, tiles_j;            // of the result (symmetric ones: tiles_i each way)
-    int blocks;                      // 64 deep blocks of the reduction
+    int count, rows, cols, m, ldx, ldm, steps;
+    int b_plane;                     // of B's first numbers: 1, or 2 where A has second ones
+    uint32_t sym_tiles, step_tiles, step_cols;       // of a matrix: tiles of A or B, of X; columns of tiles of X
+    int gram_blocks, m_blocks;       // 64 deep blocks of A's reduction, and of the others
     int tall, out_bf16;
     float scale;
     int32_t* status_word;
 };
 
-struct OrthoTile {
-    int matrix, i, j;
+// a product's tile: rows 128 i and columns kWidth j of matrix `matrix`'s A, B or next X
+struct OrthoItem {
+    int step, mode, matrix, i, j;
+    int32_t need;                    // of done[matrix]
 };
-template <int kMode>
-__device__ __forceinline__ OrthoTile ortho_tile(const OrthoParams& p, uint32_t q, uint32_t per) {
-    OrthoTile t;
-    t.matrix = (int)(q / per);
-    uint32_t r = q - (uint32_t)t.matrix * per;
-    if constexpr (kMode == kStep) {
-        t.i = (int)(r / (uint32_t)p.tiles_j);
-        t.j = (int)(r % (uint32_t)p.tiles_j);
-    } else {                                                         // columns of the upper triangle: j + 1 tiles in column j
-        int j = (int)((sqrtf(8.f * (float)r + 1.f) - 1.f) * 0.5f);
-        while ((uint32_t)(j + 1) * (uint32_t)(j + 2) / 2 <= r) ++j;
-        while ((uint32_t)j * (uint32_t)(j + 1) / 2 > r) --j;
-        t.j = j;
-        t.i = (int)(r - (uint32_t)j * (uint32_t)(j + 1) / 2);
+template <int kWidth>
+__device__ __forceinline__ OrthoItem ortho_item(const OrthoParams& p, uint32_t q) {
+    OrthoItem t;
+    const uint32_t sym = p.sym_tiles * (uint32_t)p.count, per_step = 2 * sym + p.step_tiles * (uint32_t)p.count;
+    t.step = (int)(q / per_step);
+    uint32_t r = q - (uint32_t)t.step * per_step;
+    const uint32_t matrix_tiles = 2 * p.sym_tiles + p.step_tiles;
+    if (r < 2 * sym) {
+        t.mode = r < sym ? kGram : kPoly;
+        if (t.mode == kPoly) r -= sym;
+        t.matrix = (int)(r / p.sym_tiles);
+        r -= (uint32_t)t.matrix * p.sym_tiles;
+        // column j has the tiles that reach the diagonal or lie above it: 128 j .. wide tiles j + 1 of them, 256 wide ones 2 j + 2
+        constexpr uint32_t kF = kWidth / kTile;
+        uint32_t j = (uint32_t)((sqrtf(8.f / kF * (float)r + 1.f) - 1.f) * 0.5f);
+        while (kF * (j + 1) * (j + 2) / 2 <= r) ++j;
+        while (kF * j * (j + 1) / 2 > r) --j;
+        t.j = (int)j;
+        t.i = (int)(r - kF * j * (j + 1) / 2);
+        t.need = (int)((uint32_t)t.step * matrix_tiles + (t.mode == kPoly ? p.sym_tiles : 0u));
+    } else {
+        t.mode = kStep;
+        r -= 2 * sym;
+        t.matrix = (int)(r / p.step_tiles);
+        r -= (uint32_t)t.matrix * p.step_tiles;
+        t.i = (int)(r / p.step_cols);
+        t.j = (int)(r % p.step_cols);
+        t.need = (int)((uint32_t)t.step * matrix_tiles + 2 * p.sym_tiles);
     }
     return t;
+}
+
+// Waits (bounded, as every wait here) until `need` tiles of a matrix are finished; what they wrote is then visible to this
+// thread, and to what it hands the item to, copies by TMA included.
+__device__ __forceinline__ bool wait_done(const int32_t* done, int32_t need, volatile int* abort_flag, int32_t* status_word) {
+    int32_t v;
+    uint64_t t0 = 0;
+    for (uint32_t spins = 0;; ++spins) {
+        // (an acquiring load here, over and over, would empty the SM's L1 each time and hold up the other warps' loads)
+        asm volatile("ld.relaxed.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(done) : "memory");
+        if (v >= need) break;
+        __nanosleep(64);
+        if (*abort_flag) return false;
+        if (spins == 0) t0 = ptx::global_timer_ns();
+        else if ((spins & 63u) == 0u && ptx::global_timer_ns() - t0 > ptx::kWaitLimitNs) {
+            *abort_flag = 1;
+            report_device_error(status_word, SBP_ERR_TIMEOUT);
+            return false;
+        }
+    }
+    asm volatile("fence.acq_rel.gpu;\n\tfence.proxy.async;" ::: "memory");
+    return true;
+}
+// Block `k` of a tile's sum: which 64 deep block of the reduction, from which planes.  A step in fp16 makes B X, B = a + b A + c A^2,
+// of the first numbers, and of the 128 rows and columns of B around its diagonal, whose second numbers are kept as well, also
+// first x second and second x first: that is a X to 22 bits.  These, and the blocks of the diagonal itself, come last: the tensor
+// core cuts its running sum, which is small until then.
+struct OrthoBlock {
+    int at;                          // 64 deep block
+    int second_x, second_s;          // second numbers of X, of B
+    int narrow;                      // 0: the tile's columns, 1 + h: columns 128 h .. + 127 of it
+};
+template <int kWidth>
+__device__ __forceinline__ int step_extras(const OrthoParams& p) { return p.tall ? 4 * (kWidth / kTile) : 4; }
+template <int kWidth>
+__device__ __forceinline__ OrthoBlock step_block(const OrthoParams& p, const OrthoItem& t, int k) {
+    constexpr int kF = kWidth / kTile;
+    const int len = p.tall ? 2 * kF : 2, lo = p.tall ? 2 * kF * t.j : 2 * t.i, hi = lo + len < p.m_blocks ? lo + len : p.m_blocks;
+    // (the first block has all columns of the tile: where there are no other blocks, the diagonal's come first)
+    const int others = p.m_blocks - (hi - lo), extras = step_extras<kWidth>(p), first = others > 0 ? others : hi - lo;
+    OrthoBlock b = {k < lo || others == 0 ? k : k + (hi - lo), 0, 0, 0};
+    if (k >= first + extras) {
+        b.at = lo + (k - first - extras);
+    } else if (k >= first) {
+        const int e = k - first;
+        b.at = lo + (e >> 1);                                        // (past the matrix: zeros)
+        b.second_x = e & 1;
+        b.second_s = b.second_x ^ 1;
+        if (p.tall && kF > 1) b.narrow = 1 + (e >> 2);
+    }
+    return b;
 }
 
 __device__ __forceinline__ void unpack_half(const uint4& q, float* f) {
@@ -111,13 +184,426 @@ __device__ __forceinline__ uint4 pack_half(float* f) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 
-template <int kMode, bool kExact>
-__global__ void __launch_bounds__(kOrthoThreads, 1)
-ortho_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const OrthoParams p) {
+// eight numbers of a result's row, from column `col` on
+__device__ __forceinline__ void put_result(const OrthoParams& p, int64_t row, int col, const float (&v)[8]) {
+    const int64_t o = row * p.cols + col;
+    const float k = p.scale * kDown;
+    if (p.out_bf16) {
+        __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + o;
+        if (p.cols % 8 == 0) {
+            if (col >= p.cols) return;
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * e] * k, v[2 * e + 1] * k);
+                w[e] = *reinterpret_cast<const uint32_t*>(&b);
+            }
+            *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < p.cols) out[e] = __float2bfloat16_rn(v[e] * k);
+        }
+    } else {
+        float* out = static_cast<float*>(p.out) + o;
+        if (p.cols % 4 == 0) {
+#pragma unroll
+            for (int e = 0; e < 8; e += 4)
+                if (col + e < p.cols) *reinterpret_cast<float4*>(out + e) = make_float4(v[e] * k, v[e + 1] * k, v[e + 2] * k, v[e + 3] * k);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+                if (col + e < p.cols) out[e] = v[e] * k;
+        }
+    }
+}
+
+// An accumulator's turns: which of two is next, and which of its phases.
+struct Turns {
+    uint32_t used = 0;
+    __device__ __forceinline__ uint32_t slot() const { return used & 1u; }
+    __device__ __forceinline__ uint32_t phase() const { return (used >> 1) & 1u; }
+};
+
+struct OrthoWarp {                   // what an epilogue warp works with
+    OrthoControl* ctl;
+    uint8_t* staging;
+    volatile int* abort_flag;
+    uint32_t tmem;                   // of its quarter of the accumulators' rows
+    int lane, quad, half;
+    Turns acc, small;
+};
+
+// Waits for the sums of the next part; hands back an accumulator that has been read.
+__device__ __forceinline__ bool take_sums(OrthoWarp& w, uint64_t* full, const Turns& t, int32_t* status_word) {
+    bool ok = true;
+    if (w.lane == 0) ok = ptx::mbar_wait(ptx::smem_addr(&full[t.slot()]), t.phase(), w.abort_flag, status_word);
+    ok = __all_sync(0xffffffffu, ok);
+    ptx::tc_fence_after_sync();
+    return ok;
+}
+__device__ __forceinline__ void give_back(OrthoWarp& w, uint64_t* empty, Turns& t) {
+    ptx::tc_fence_before_sync();
+    __syncwarp();
+    if (w.lane == 0) ptx::mbar_arrive(ptx::smem_addr(&empty[t.slot()]));
+    ++t.used;
+}
+
+// The epilogue of one tile by one warp where the products take both numbers of every operand: 32 rows, 64 columns, 32 at a time.
+// The sums of the parts are added up in registers, then combined with numbers from memory.
+template <int kMode>
+__device__ __forceinline__ bool ortho_epilogue_exact(const OrthoParams& p, const OrthoItem& t, OrthoWarp& w) {
+    constexpr bool kSymmetric = kMode != kStep;
+    constexpr int kWidth = kTile, kCols = 64, kChunks = 2;
+    const int lane = w.lane, sub = lane >> 2, ch = lane & 3;
+    const int rows = kSymmetric ? p.m : p.rows, ld = kSymmetric ? p.ldm : p.ldx;
+    const int row0 = t.i * kTile + w.quad * 32, col0 = t.j * kWidth + w.half * kCols;
+    const int64_t s_all = (int64_t)p.count * p.s_plane, x_all = (int64_t)p.count * p.x_plane;
+    __half* S = p.S + (int64_t)t.matrix * p.s_plane;                 // (first numbers of A)
+    __half* X = p.X + (int64_t)t.matrix * p.x_plane;
+    float* diag_a = p.diag_a + (int64_t)t.matrix * p.ldm;
+    float* diag_b = p.diag_b + (int64_t)t.matrix * p.ldm;
+    const __half* from = kMode == kPoly ? S : X + (int64_t)(t.step & 1) * 2 * x_all;
+    __half* to = kMode == kGram ? S : kMode == kPoly ? S + p.b_plane * s_all : X + (int64_t)((t.step & 1) ^ 1) * 2 * x_all;
+    const int64_t from_second = kMode == kPoly ? s_all : x_all, to_second = kMode == kStep ? x_all : s_all;
+    constexpr bool kCombine = kMode != kGram;
+    const bool last = kMode == kStep && t.step == p.steps - 1;
+    const bool mirrored = kSymmetric && t.j > t.i;
+
+    // what the sums are combined with is asked for a chunk ahead (columns between the matrix's and its pitch are written and never
+    // read); past the L1, which may hold an earlier step's numbers
+    uint4 first_q[2][4], second_q[2][4];
+    float f[2][8];                                              // step: a + the diagonal of B; second product: the diagonal of A
+    auto ask = [&](int c, int b) {
+        const int col = col0 + c * 32 + ch * 8;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int row = row0 + i * 8 + sub;
+            const bool in = row < rows && col < ld;
+            const int64_t at = (int64_t)row * ld + col;
+            if constexpr (kCombine) first_q[b][i] = in ? __ldcg(reinterpret_cast<const uint4*>(from + at)) : make_uint4(0u, 0u, 0u, 0u);
+            if constexpr (kCombine) second_q[b][i] = in ? __ldcg(reinterpret_cast<const uint4*>(from + from_second + at)) : make_uint4(0u, 0u, 0u, 0u);
+            if (kMode == kStep && !p.tall) f[b][i] = in ? kNsA + __ldcg(diag_b + row) : 0.f;
+            if (kMode == kPoly) f[b][i] = in && t.j == t.i ? __ldcg(diag_a + row) : 0.f;
+        }
+        if (kMode == kStep && p.tall) {                              // one for each column (ld and ldm are the same here)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[b][e] = col < ld ? kNsA + __ldcg(diag_b + col + e) : 0.f;
+        }
+    };
+    if constexpr (kMode != kGram) {
+        ask(0, 0);
+    }
+    float sum[kCols];
+#pragma unroll
+    for (int i = 0; i < kCols; ++i) sum[i] = 0.f;
+    {
+        const int blocks = kMode == kGram ? p.gram_blocks : p.m_blocks;
+        auto add = [&](uint32_t taddr) {
+#pragma unroll
+            for (int c = 0; c < kCols; c += 32) {
+                float v[32];
+                ptx::tmem_ld_32x32(taddr + c, v);
+                ptx::tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) sum[c + i] += v[i];
+            }
+        };
+        for (int part = 0; part < blocks; part += kPartBlocks) {
+            if (!take_sums(w, w.ctl->acc_full, w.acc, p.status_word)) return false;
+            add(w.tmem + w.acc.slot() * kWidth + w.half * kCols);
+            give_back(w, w.ctl->acc_empty, w.acc);
+        }
+        if (!take_sums(w, w.ctl->small_full, w.small, p.status_word)) return false;
+        add(w.tmem + (2 + w.small.slot()) * kWidth + w.half * kCols);
+        give_back(w, w.ctl->small_empty, w.small);
+    }
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        if (kCombine && c + 1 < kChunks) ask(c + 1, c + 1);
+        // a lane has one row of the accumulator: through shared memory into rows of four lanes
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            const float* v = &sum[c * 32 + 4 * g];
+            *reinterpret_cast<float4*>(w.staging + lane * 128 + ((g ^ (lane & 7)) << 4)) = make_float4(v[0], v[1], v[2], v[3]);
+        }
+        __syncwarp();
+        const int col = col0 + c * 32 + ch * 8;
+        uint4 first_out[4], second_out[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int r = i * 8 + sub, row = row0 + r;
+            float v[8];
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const float4 x = *reinterpret_cast<const float4*>(w.staging + r * 128 + (((2 * ch + h) ^ (r & 7)) << 4));
+                v[4 * h] = x.x;
+                v[4 * h + 1] = x.y;
+                v[4 * h + 2] = x.z;
+                v[4 * h + 3] = x.w;
+            }
+            const bool in = row < rows && col < ld;
+            const int64_t at = (int64_t)row * ld + col;
+            float first[8] = {}, second[8] = {};
+            if constexpr (kCombine) {
+                unpack_half(first_q[c][i], first);
+                unpack_half(second_q[c][i], second);
+            }
+            if constexpr (kMode == kGram) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    v[e] *= kDown;                                   // 2^24 A as it comes, 2^12 A as it is held
+                    if (in && row == col + e) diag_a[row] = v[e] * kDown;
+                }
+            } else if constexpr (kMode == kPoly) {
+                // the diagonal in fp32: A_ii as its product left it, and (A^2)_ii with that in A_ii's place
+                const float d = f[c][i];
+                float on_diagonal = 0.f;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float a2 = v[e] * (kDown * kDown), h = first[e] * kDown, l = second[e] * kDown;
+                    v[e] = fmaf(kNsB, first[e] + second[e], kNsC * a2 * kUp);
+                    if (row == col + e) {
+                        on_diagonal = kNsB * d + kNsC * (a2 + (d - h) * (d + h) - 2.f * h * l);
+                        v[e] = 0.f;
+                    }
+                }
+                if (in && row >= col && row < col + 8) diag_b[row] = on_diagonal;
+            } else {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float k = p.tall ? f[c][e] : f[c][i];
+                    v[e] = fmaf(k, second[e], fmaf(k, first[e], v[e] * kDown));
+                }
+            }
+            if (last) {
+                if (row < p.rows) put_result(p, (int64_t)t.matrix * p.rows + row, col, v);
+            } else {
+                first_out[i] = pack_half(v);
+                second_out[i] = pack_half(v);
+                if (in) {
+                    *reinterpret_cast<uint4*>(to + at) = first_out[i];
+                    *reinterpret_cast<uint4*>(to + to_second + at) = second_out[i];
+                }
+            }
+        }
+        __syncwarp();
+        if (mirrored) {                                              // the other way: 32 rows of 32, 16-byte pieces swizzled
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const uint32_t a[4] = {first_out[i].x, first_out[i].y, first_out[i].z, first_out[i].w};
+                const uint32_t b[4] = {second_out[i].x, second_out[i].y, second_out[i].z, second_out[i].w};
+                uint8_t* m = w.staging + ch * 512 + ((i ^ ch) << 4) + sub * 2;
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    *reinterpret_cast<uint16_t*>(m + e * 64) = (uint16_t)(a[e >> 1] >> (16 * (e & 1)));
+                    *reinterpret_cast<uint16_t*>(m + kHalfBytes + e * 64) = (uint16_t)(b[e >> 1] >> (16 * (e & 1)));
+                }
+            }
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = col0 + c * 32 + i * 8 + sub, at_col = row0 + ch * 8;
+                const uint8_t* m = w.staging + (i * 8 + sub) * 64 + ((ch ^ i) << 4);
+                if (row < p.m && at_col < p.ldm) {
+                    const int64_t at = (int64_t)row * p.ldm + at_col;
+                    *reinterpret_cast<uint4*>(to + at) = *reinterpret_cast<const uint4*>(m);
+                    *reinterpret_cast<uint4*>(to + s_all + at) = *reinterpret_cast<const uint4*>(m + kHalfBytes);
+                }
+            }
+            __syncwarp();
+        }
+    }
+    return true;
+}
+
+// 32 x 32 numbers of a bf16 result, a row a lane, into the output (fp32 ones take both numbers of every operand).
+__device__ __forceinline__ void put_results(const OrthoParams& p, int matrix, int row0, int c0, const float (&v)[32], OrthoWarp& w) {
+    const int lane = w.lane;
+    if (p.cols % 8 != 0) {                                           // rows that begin anywhere
+        if (row0 + lane < p.rows) {
+            const int64_t o = ((int64_t)matrix * p.rows + row0 + lane) * p.cols + c0;
+#pragma unroll
+            for (int e = 0; e < 32; ++e) {
+                if (c0 + e >= p.cols) continue;
+                static_cast<__nv_bfloat16*>(p.out)[o + e] = __float2bfloat16_rn(v[e]);
+            }
+        }
+        return;
+    }
+    uint32_t b[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+        const __nv_bfloat162 h = __floats2bfloat162_rn(v[2 * e], v[2 * e + 1]);
+        b[e] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+        *reinterpret_cast<uint4*>(w.staging + lane * 64 + ((g ^ ((lane >> 1) & 3)) << 4)) = make_uint4(b[4 * g], b[4 * g + 1], b[4 * g + 2], b[4 * g + 3]);
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int r = i * 8 + (lane >> 2), row = row0 + r, col = c0 + (lane & 3) * 8;
+        if (row < p.rows && col < p.cols)
+            *reinterpret_cast<uint4*>(static_cast<__nv_bfloat16*>(p.out) + ((int64_t)matrix * p.rows + row) * p.cols + col) =
+                *reinterpret_cast<const uint4*>(w.staging + r * 64 + (((lane & 3) ^ ((r >> 1) & 3)) << 4));
+    }
+    __syncwarp();
+}
+
+// The epilogue where the products take the first numbers: kCols columns of 32 rows, a row a lane.  The next X has its a X in the sums
+// already; the second product's sums are combined with A.
+template <int kMode, int kWidth, int kCols>
+__device__ __forceinline__ bool ortho_epilogue(const OrthoParams& p, const OrthoItem& t, OrthoWarp& w) {
+    constexpr bool kSymmetric = kMode != kStep;
+    constexpr int kChunks = kCols / 32;
+    const int lane = w.lane, sub = lane >> 2, ch = lane & 3;
+    const int rows = kSymmetric ? p.m : p.rows, ld = kSymmetric ? p.ldm : p.ldx;
+    const int row0 = t.i * kTile + w.quad * 32, col0 = t.j * kWidth + w.half * kCols;
+    const int64_t s_all = (int64_t)p.count * p.s_plane, x_all = (int64_t)p.count * p.x_plane;
+    __half* S = p.S + (int64_t)t.matrix * p.s_plane;
+    __half* to = kMode == kGram ? S : kMode == kPoly ? S + p.b_plane * s_all
+                                                     : p.X + (int64_t)((t.step & 1) ^ 1) * 2 * x_all + (int64_t)t.matrix * p.x_plane;
+    float* diag_a = p.diag_a + (int64_t)t.matrix * p.ldm;
+    const bool last = kMode == kStep && t.step == p.steps - 1;
+    // below the diagonal a wide tile's half repeats what another tile stores
+    const int block_j = col0 / kTile;
+    const bool below = kSymmetric && block_j < t.i, mirrored = kSymmetric && block_j > t.i, on_diagonal = kSymmetric && block_j == t.i;
+    const bool put_second = kMode == kStep || (kMode == kPoly && on_diagonal);
+    // 64 bytes a row, 16-byte pieces swizzled: a row a lane, and rows of four lanes
+    auto own = [&](int g) { return reinterpret_cast<uint4*>(w.staging + lane * 64 + ((g ^ ((lane >> 1) & 3)) << 4)); };
+    auto shared = [&](int i) {
+        const int r = i * 8 + sub;
+        return reinterpret_cast<uint4*>(w.staging + r * 64 + ((ch ^ ((r >> 1) & 3)) << 4));
+    };
+    // A is asked for before the sums are there; past the L1, which may hold an earlier step's numbers
+    uint4 a_q[kMode == kPoly ? kChunks : 1][4];
+    float d = 0.f;
+    if constexpr (kMode == kPoly) {
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = row0 + i * 8 + sub, col = col0 + c * 32 + ch * 8;
+                a_q[c][i] = row < rows && col < ld && !below ? __ldcg(reinterpret_cast<const uint4*>(S + (int64_t)row * ld + col))
+                                                             : make_uint4(0u, 0u, 0u, 0u);
+            }
+        if (on_diagonal && row0 + lane < p.m) d = __ldcg(diag_a + row0 + lane);
+    }
+    if (!take_sums(w, w.ctl->acc_full, w.acc, p.status_word)) return false;
+    const uint32_t taddr = w.tmem + w.acc.slot() * kWidth + w.half * kCols;
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) {
+        float v[32];
+        ptx::tmem_ld_32x32(taddr + c * 32, v);
+        ptx::tmem_ld_wait();
+        if (c == kChunks - 1) give_back(w, w.ctl->acc_empty, w.acc);
+        const int c0 = col0 + c * 32;
+        if (below || c0 >= ld || row0 >= rows) continue;
+        // 2^24 times the sum as it comes; 2^12 as it is held
+        if (last) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] *= p.scale * (kDown * kDown);
+            put_results(p, t.matrix, row0, c0, v, w);
+            continue;
+        }
+        if constexpr (kMode == kPoly) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) *shared(i) = a_q[c][i];
+            __syncwarp();
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                float a[8];
+                unpack_half(*own(g), a);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const float s = v[8 * g + e];
+                    v[8 * g + e] = fmaf(kNsB, a[e], kNsC * kDown * s);
+                    if (c0 == row0 && 8 * g + e == lane) {
+                        // the diagonal of B, a included, from A_ii in fp32: as its product left it, and in its place in (A^2)_ii
+                        const float h = a[e] * kDown;
+                        v[8 * g + e] = (kNsA + kNsB * d + kNsC * (s * (kDown * kDown) + (d - h) * (d + h))) * kUp;
+                    }
+                }
+            }
+            __syncwarp();
+        } else {
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] *= kDown;
+            if (kMode == kGram && c0 == row0) {
+#pragma unroll
+                for (int e = 0; e < 32; ++e) d = e == lane ? v[e] : d;
+                if (row0 + lane < p.m) diag_a[row0 + lane] = d * kDown;
+            }
+        }
+        uint32_t first[16];
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+            const __half2 h = __floats2half2_rn(v[2 * e], v[2 * e + 1]);
+            first[e] = *reinterpret_cast<const uint32_t*>(&h);
+            if constexpr (kMode != kGram) {
+                const float2 r = __half22float2(h);
+                v[2 * e] -= r.x;
+                v[2 * e + 1] -= r.y;
+            }
+        }
+        auto put = [&](const uint32_t (&x)[16], __half* plane) {
+#pragma unroll
+            for (int g = 0; g < 4; ++g) *own(g) = make_uint4(x[4 * g], x[4 * g + 1], x[4 * g + 2], x[4 * g + 3]);
+            __syncwarp();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int row = row0 + i * 8 + sub, col = c0 + ch * 8;
+                if (row < rows && col < ld) *reinterpret_cast<uint4*>(plane + (int64_t)row * ld + col) = *shared(i);
+            }
+            __syncwarp();
+        };
+        put(first, to);
+        if (kMode != kGram && put_second) {
+            uint32_t second[16];
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const __half2 h = __floats2half2_rn(v[2 * e], v[2 * e + 1]);
+                second[e] = *reinterpret_cast<const uint32_t*>(&h);
+            }
+            put(second, to + (kMode == kStep ? x_all : s_all));
+        }
+        if (mirrored) {
+            // the other way: two lanes have rows r, r + 1 of columns c, c + 1; after an exchange one has column c of both, the
+            // other column c + 1, and 16 lanes store 64 bytes
+            const int col = row0 + (lane & ~1);
+#pragma unroll
+            for (int e = 0; e < 16; ++e) {
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, first[e], 1);
+                const uint32_t pair = lane & 1 ? __byte_perm(other, first[e], 0x7632) : __byte_perm(first[e], other, 0x5410);
+                const int row = c0 + 2 * e + (lane & 1);
+                if (row < p.m && col < p.ldm) *reinterpret_cast<uint32_t*>(to + (int64_t)row * p.ldm + col) = pair;
+            }
+        }
+    }
+    return true;
+}
+
+// Epilogue warps: their loads, stores and fences take longer than their arithmetic, so sixteen, as many as the registers allow; eight
+// where the sums are added up in registers.
+__host__ __device__ constexpr int ortho_epilogue_warps(bool exact) { return exact ? 8 : 16; }
+__host__ __device__ constexpr int ortho_threads(bool exact) { return 32 * (kFirstEpilogueWarp + ortho_epilogue_warps(exact)); }
+
+// kExact: both numbers of every operand, three products; kWidth: columns of a tile.
+template <bool kExact, int kWidth>
+__global__ void __launch_bounds__(ortho_threads(kExact), 1)
+ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__ CUtensorMap x_across, const __grid_constant__ CUtensorMap s_rows,
+             const OrthoParams p) {
+    static_assert(!kExact || kWidth == kTile, "the sums in registers have room for 128 columns");
+    constexpr uint32_t kPlane = kOperand + kWidth * kRow, kStage = (kExact ? 2 : 1) * kPlane;
+    constexpr int kStages = kRing / kStage;
+    static_assert(kStages <= kMostStages, "stages");
+    constexpr uint32_t kTmemCols = (kExact ? 4 : 2) * kWidth;
+    constexpr int kEpilogueWarps = ortho_epilogue_warps(kExact), kCols = kWidth / (kEpilogueWarps / 4);
     extern __shared__ uint8_t smem_raw[];
     const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31;
     const uint32_t raw = ptx::smem_addr(smem_raw), ring = (raw + 1023u) & ~1023u;
-    OrthoControl* ctl = reinterpret_cast<OrthoControl*>(smem_raw + (ring - raw) + kStages * kStage);
+    OrthoControl* ctl = reinterpret_cast<OrthoControl*>(smem_raw + (ring - raw) + kRing);
 
     pdl_launch_dependents();
     if (threadIdx.x == 0) {
@@ -127,14 +613,22 @@ ortho_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
         }
         for (int a = 0; a < 2; ++a) {
             ptx::mbar_init(ptx::smem_addr(&ctl->acc_full[a]), 1);
-            ptx::mbar_init(ptx::smem_addr(&ctl->acc_empty[a]), 4);
+            ptx::mbar_init(ptx::smem_addr(&ctl->acc_empty[a]), kEpilogueWarps);
+            ptx::mbar_init(ptx::smem_addr(&ctl->small_full[a]), 1);
+            ptx::mbar_init(ptx::smem_addr(&ctl->small_empty[a]), kEpilogueWarps);
+        }
+        for (int i = 0; i < kItems; ++i) {
+            ptx::mbar_init(ptx::smem_addr(&ctl->item_full[i]), 1);
+            ptx::mbar_init(ptx::smem_addr(&ctl->item_empty[i]), kEpilogueWarps + 3);
+            ptx::mbar_init(ptx::smem_addr(&ctl->stored[i]), kEpilogueWarps);
         }
         ctl->abort_flag = 0;
         ptx::fence_mbar_init();
-        ptx::prefetch_tensormap(&map_a);
-        ptx::prefetch_tensormap(&map_b);
+        ptx::prefetch_tensormap(&x_rows);
+        ptx::prefetch_tensormap(&x_across);
+        ptx::prefetch_tensormap(&s_rows);
     }
-    if (warp == 5) ptx::tmem_alloc(ptx::smem_addr(&ctl->tmem_slot), 2 * kTile);
+    if (warp == kProductWarp) ptx::tmem_alloc(ptx::smem_addr(&ctl->tmem_slot), kTmemCols);
     ptx::tc_fence_before_sync();
     __syncthreads();
     ptx::tc_fence_after_sync();
@@ -143,62 +637,70 @@ ortho_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
     int32_t* status_word = p.status_word;
     pdl_wait();
     const bool skip = status_word != nullptr && *reinterpret_cast<volatile int32_t*>(status_word) != 0;
+    const uint32_t total = (uint32_t)p.steps * (2 * p.sym_tiles + p.step_tiles) * (uint32_t)p.count;
 
-    constexpr bool kSymmetric = kMode != kStep;
-    const uint32_t per = kSymmetric ? (uint32_t)p.tiles_i * (uint32_t)(p.tiles_i + 1) / 2 : (uint32_t)p.tiles_i * (uint32_t)p.tiles_j;
-    const uint32_t total = per * (uint32_t)p.count;
-    // which operands are read across (their reduction runs along rows of X): both of a tall matrix's A, X of a wide one's step
-    const bool across_a = kMode == kGram && p.tall, across_b = across_a || (kMode == kStep && !p.tall);
-    // the parts of a tile's sum: (block, operands' planes) in the order of issue; exact: second x first, first x second, first x first
-    const int terms = kExact ? 3 : 1;
-    const int all_blocks = terms * p.blocks;
-    const int small = kExact ? 2 * p.blocks : 0;                     // blocks of the small products, one part
-    auto part_end = [&](int k) {                                     // whether block k is a part's last one
-        if (k == all_blocks - 1) return true;
-        return kExact && (k == small - 1 || (k >= small && (k - small) % kPartBlocks == kPartBlocks - 1));
+    // the item in the ring's next place, for the warps that do not draw; false where a wait ran out
+    auto next_item = [&](uint32_t n, uint32_t& q, bool free_place = true) {
+        const uint32_t s = n % kItems;
+        bool ok = ptx::mbar_wait(ptx::smem_addr(&ctl->item_full[s]), (n / kItems) & 1u, abort_flag, status_word);
+        ok = __all_sync(0xffffffffu, ok);
+        q = *reinterpret_cast<volatile uint32_t*>(&ctl->item[s]);
+        __syncwarp();
+        if (free_place && lane == 0) ptx::mbar_arrive(ptx::smem_addr(&ctl->item_empty[s]));
+        return ok;
     };
 
     if (skip) {
         // an earlier call failed: the outputs are left alone
-    } else if (warp == 4) {
+    } else if (warp == kCopyWarp) {
         const bool leader = ptx::elect_one();
         uint32_t it = 0;
         bool ok = true;
-        for (uint32_t q = blockIdx.x; q < total && ok; q += gridDim.x) {
-            const OrthoTile t = ortho_tile<kMode>(p, q, per);
-            for (int k = 0; k < all_blocks; ++k, ++it) {
-                const int term = kExact ? k / p.blocks : 2, y = (kExact ? k % p.blocks : k) * kDeep;
-                const int second_a = term == 0 ? 1 : 0, second_b = term == 1 ? 1 : 0;
-                int za, zb;
-                if constexpr (kMode == kGram) {
-                    za = (p.buffer * 2 + second_a) * p.count + t.matrix;
-                    zb = (p.buffer * 2 + second_b) * p.count + t.matrix;
-                } else if constexpr (kMode == kPoly) {
-                    za = second_a * p.count + t.matrix;
-                    zb = second_b * p.count + t.matrix;
-                } else {
-                    const int zx = (p.buffer * 2 + (p.tall ? second_a : second_b)) * p.count + t.matrix;
-                    const int zs = (p.s_planes + (p.tall ? second_b : second_a)) * p.count + t.matrix;
-                    za = p.tall ? zx : zs;
-                    zb = p.tall ? zs : zx;
-                }
-                const int s = it % kStages;
+        for (uint32_t n = 0; ok; ++n) {
+            uint32_t q;
+            ok = next_item(n, q);
+            if (!ok || q >= total) break;
+            const OrthoItem t = ortho_item<kWidth>(p, q);
+            // which operands are read across: both of a tall matrix's A (its reduction runs down X), X of a wide one's step
+            const bool across_a = t.mode == kGram && p.tall, across_b = across_a || (t.mode == kStep && !p.tall);
+            const bool a_is_x = t.mode == kGram || (t.mode == kStep && p.tall), b_is_x = t.mode == kGram || (t.mode == kStep && !p.tall);
+            const CUtensorMap* map_a = a_is_x ? (across_a ? &x_across : &x_rows) : &s_rows;
+            const CUtensorMap* map_b = b_is_x ? (across_b ? &x_across : &x_rows) : &s_rows;
+            const int x_first = (t.step & 1) * 2, s_first = t.mode == kStep ? p.b_plane : 0;
+            const int za = (a_is_x ? x_first : s_first) * p.count + t.matrix, zb = (b_is_x ? x_first : s_first) * p.count + t.matrix;
+            const bool with_extras = !kExact && t.mode == kStep;
+            const int blocks = t.mode == kGram ? p.gram_blocks : p.m_blocks + (with_extras ? step_extras<kWidth>(p) : 0);
+            for (int k = 0; k < blocks && ok; ++k, ++it) {
+                const OrthoBlock blk = with_extras ? step_block<kWidth>(p, t, k) : OrthoBlock{k, 0, 0, 0};
+                const int y = blk.at * kDeep;
+                const uint32_t s = it % kStages;
                 ok = ptx::mbar_wait(ptx::smem_addr(&ctl->empty[s]), ((it / kStages) & 1u) ^ 1u, abort_flag, status_word);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
-                const uint32_t full = ptx::smem_addr(&ctl->full[s]), a = ring + s * kStage, b = a + kOperand;
-                if (leader) ptx::mbar_arrive_expect_tx(full, kStage);
-                if (across_a) {
-                    ptx::tma_load_3d_warp(a, &map_a, t.i * kTile, y, za, full, leader);
-                    ptx::tma_load_3d_warp(a + kHalfOperand, &map_a, t.i * kTile + 64, y, za, full, leader);
-                } else {
-                    ptx::tma_load_3d_warp(a, &map_a, y, t.i * kTile, za, full, leader);
-                }
-                if (across_b) {
-                    ptx::tma_load_3d_warp(b, &map_b, t.j * kTile, y, zb, full, leader);
-                    ptx::tma_load_3d_warp(b + kHalfOperand, &map_b, t.j * kTile + 64, y, zb, full, leader);
-                } else {
-                    ptx::tma_load_3d_warp(b, &map_b, y, t.j * kTile, zb, full, leader);
+                const uint32_t full = ptx::smem_addr(&ctl->full[s]);
+                if (leader) ptx::mbar_arrive_expect_tx(full, blk.narrow ? 2 * kOperand : kStage);
+#pragma unroll
+                for (int second = 0; second < (kExact ? 2 : 1); ++second) {
+                    const uint32_t a = ring + s * kStage + second * kPlane, b = a + kOperand;
+                    const int z_a = za + (second + (a_is_x ? blk.second_x : blk.second_s)) * p.count;
+                    const int z_b = zb + (second + (b_is_x ? blk.second_x : blk.second_s)) * p.count;
+                    if (across_a) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) ptx::tma_load_3d_warp(a + h * kHalfOperand, map_a, t.i * kTile + 64 * h, y, z_a, full, leader);
+                    } else {
+                        ptx::tma_load_3d_warp(a, map_a, y, t.i * kTile, z_a, full, leader);
+                    }
+                    if (across_b) {
+#pragma unroll
+                        for (int h = 0; h < kWidth / 64; ++h)
+                            ptx::tma_load_3d_warp(b + h * kHalfOperand, map_b, t.j * kWidth + 64 * h, y, z_b, full, leader);
+                    } else if (blk.narrow) {
+                        ptx::tma_load_3d_warp(b, map_b, y, t.j * kWidth + kTile * (blk.narrow - 1), z_b, full, leader);
+                    } else {
+#pragma unroll
+                        for (int h = 0; h < kWidth / kTile; ++h)
+                            ptx::tma_load_3d_warp(b + h * kOperand, map_b, y, t.j * kWidth + kTile * h, z_b, full, leader);
+                    }
                 }
             }
         }
@@ -210,260 +712,138 @@ ortho_product_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_con
             }
         }
         __syncwarp();
-    } else if (warp == 5) {
+    } else if (warp == kProductWarp) {
         const bool leader = ptx::elect_one();
-        uint32_t it = 0, used = 0;
+        uint32_t it = 0;
+        Turns acc, small;
         bool ok = true;
-        const uint32_t idesc = ptx::umma_idesc_f16(kTile, kTile, across_a, across_b);
-        const uint32_t a_step = (across_a ? kUmmaDeep * kRow : kUmmaDeep * 2u) >> 4, b_step = (across_b ? kUmmaDeep * kRow : kUmmaDeep * 2u) >> 4;
-        const uint32_t a_lo = ptx::umma_desc_lo(ring, across_a ? kHalfOperand : 16u);
-        const uint32_t b_lo = ptx::umma_desc_lo(ring + kOperand, across_b ? kHalfOperand : 16u);
-        for (uint32_t q = blockIdx.x; q < total && ok; q += gridDim.x) {
-            bool fresh = true;
-            for (int k = 0; k < all_blocks; ++k, ++it) {
-                const uint32_t acc = used & 1u;
-                if (fresh) {
-                    ok = ptx::mbar_wait(ptx::smem_addr(&ctl->acc_empty[acc]), ((used >> 1) & 1u) ^ 1u, abort_flag, status_word);
-                    ok = __all_sync(0xffffffffu, ok);
-                    if (!ok) break;
-                }
+        for (uint32_t n = 0; ok; ++n) {
+            uint32_t q;
+            ok = next_item(n, q);
+            if (!ok || q >= total) break;
+            const OrthoItem t = ortho_item<kWidth>(p, q);
+            const bool across_a = t.mode == kGram && p.tall, across_b = across_a || (t.mode == kStep && !p.tall);
+            const bool with_extras = !kExact && t.mode == kStep;
+            const int blocks = t.mode == kGram ? p.gram_blocks : p.m_blocks + (with_extras ? step_extras<kWidth>(p) : 0);
+            const uint32_t idesc = ptx::umma_idesc_f16(kTile, kWidth, across_a, across_b);
+            const uint32_t a_step = (across_a ? kUmmaDeep * kRow : kUmmaDeep * 2u) >> 4, b_step = (across_b ? kUmmaDeep * kRow : kUmmaDeep * 2u) >> 4;
+            const uint32_t a_lo = ptx::umma_desc_lo(ring, across_a ? kHalfOperand : 16u);
+            const uint32_t b_lo = ptx::umma_desc_lo(ring + kOperand, across_b ? kHalfOperand : 16u);
+            auto wait_empty = [&](uint64_t* empty, const Turns& turn) {
+                const bool got = ptx::mbar_wait(ptx::smem_addr(&empty[turn.slot()]), turn.phase() ^ 1u, abort_flag, status_word);
+                return (bool)__all_sync(0xffffffffu, got);
+            };
+            if (kExact) ok = wait_empty(ctl->small_empty, small);
+            for (int k = 0; k < blocks && ok; ++k, ++it) {
+                const bool fresh = kExact ? k % kPartBlocks == 0 : k == 0;
+                if (fresh && !(ok = wait_empty(ctl->acc_empty, acc))) break;
                 const uint32_t s = it % kStages;
                 ok = ptx::mbar_wait(ptx::smem_addr(&ctl->full[s]), (it / kStages) & 1u, abort_flag, status_word);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
-                const uint32_t a = a_lo + s * (kStage >> 4), b = b_lo + s * (kStage >> 4);
+                const uint32_t a = a_lo + s * (kStage >> 4), b = b_lo + s * (kStage >> 4), d = tmem + acc.slot() * kWidth;
+                if constexpr (kExact) {
+                    const uint32_t d2 = tmem + (2 + small.slot()) * kWidth, two = kPlane >> 4;
 #pragma unroll
-                for (uint32_t u = 0; u < kDeep / kUmmaDeep; ++u)
-                    ptx::umma_bf16_warp<false>(tmem + acc * kTile, ptx::umma_desc_of(a + u * a_step), ptx::umma_desc_of(b + u * b_step), idesc,
-                                               !(fresh && u == 0u), leader);
-                fresh = false;
+                    for (uint32_t u = 0; u < kDeep / kUmmaDeep; ++u) {
+                        const uint32_t au = a + u * a_step, bu = b + u * b_step;
+                        ptx::umma_bf16_warp<false>(d2, ptx::umma_desc_of(au + two), ptx::umma_desc_of(bu), idesc, (k | u) != 0u, leader);
+                        ptx::umma_bf16_warp<false>(d, ptx::umma_desc_of(au), ptx::umma_desc_of(bu), idesc, !(fresh && u == 0u), leader);
+                        ptx::umma_bf16_warp<false>(d2, ptx::umma_desc_of(au), ptx::umma_desc_of(bu + two), idesc, true, leader);
+                    }
+                } else {
+                    const int narrow = with_extras ? step_block<kWidth>(p, t, k).narrow : 0;
+                    const uint32_t di = narrow ? d + kTile * (narrow - 1) : d, id = narrow ? ptx::umma_idesc_f16(kTile, kTile, false, false) : idesc;
+#pragma unroll
+                    for (uint32_t u = 0; u < kDeep / kUmmaDeep; ++u)
+                        ptx::umma_bf16_warp<false>(di, ptx::umma_desc_of(a + u * a_step), ptx::umma_desc_of(b + u * b_step), id, (k | u) != 0u, leader);
+                }
                 if (leader) ptx::umma_commit(ptx::smem_addr(&ctl->empty[s]));
-                if (part_end(k)) {
-                    if (leader) ptx::umma_commit(ptx::smem_addr(&ctl->acc_full[acc]));
-                    ++used;
-                    fresh = true;
+                if (k == blocks - 1 || (kExact && k % kPartBlocks == kPartBlocks - 1)) {
+                    if (leader) ptx::umma_commit(ptx::smem_addr(&ctl->acc_full[acc.slot()]));
+                    ++acc.used;
+                }
+                if (kExact && k == blocks - 1) {
+                    if (leader) ptx::umma_commit(ptx::smem_addr(&ctl->small_full[small.slot()]));
+                    ++small.used;
                 }
                 __syncwarp();
             }
         }
         __syncwarp();
-    } else {
-        uint32_t used = 0;
-        bool ok = true;
-        uint8_t* staging = smem_raw + (ring - raw) + kStages * kStage + 256 + warp * kWarpBytes;
-        uint8_t* mirror = staging + kStagingBytes;
-        const int sub = lane >> 3, ch = lane & 7;
-        auto take = [&](uint32_t& taddr) {                           // the next part's sums, once they are there
-            const uint32_t acc = used & 1u;
-            if (lane == 0) ok = ptx::mbar_wait(ptx::smem_addr(&ctl->acc_full[acc]), (used >> 1) & 1u, abort_flag, status_word);
-            ok = !ptx::bar_or<kEpilogueBarrier, 128>(!ok);           // the four warps go on, or give up, together
-            ptx::tc_fence_after_sync();
-            taddr = tmem + acc * kTile + ((uint32_t)(warp * 32) << 16);
-        };
-        auto give_back = [&]() {
-            ptx::tc_fence_before_sync();
+    } else if (warp == kDrawWarp) {
+        // Draws items and waits until they are ready: the counter's and the counts' answers take 3000 clocks, half as long as a tile's
+        // products.  The ring's places allow one item beyond those being copied, multiplied and stored.
+        for (uint32_t n = 0;; ++n) {
+            const uint32_t slot = n % kItems;
+            bool ok = ptx::mbar_wait(ptx::smem_addr(&ctl->item_empty[slot]), ((n / kItems) & 1u) ^ 1u, abort_flag, status_word);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            uint32_t q = 0;
+            if (lane == 0) q = atomicAdd(p.drawn, 1u);
+            q = __shfl_sync(0xffffffffu, q, 0);
+            if (q < total && lane == 0) {
+                const OrthoItem t = ortho_item<kWidth>(p, q);
+                ok = wait_done(p.done + t.matrix, t.need, abort_flag, status_word);
+            }
+            if (!__all_sync(0xffffffffu, ok)) break;
+            if (lane == 0) {
+                *reinterpret_cast<volatile uint32_t*>(&ctl->item[slot]) = q;
+                ptx::mbar_arrive(ptx::smem_addr(&ctl->item_full[slot]));
+            }
+            if (q >= total) break;
+        }
+        __syncwarp();
+    } else if (warp == kTellWarp) {
+        // Tells the other blocks of a finished tile: a fence waits until its stores have arrived, 1.5 us, which the epilogue warps
+        // would otherwise spend.  An item's place in the ring is only freed then, so that no barrier here is passed twice.
+        for (uint32_t n = 0;; ++n) {
+            uint32_t q;
+            if (!next_item(n, q, false) || q >= total) break;
+            const OrthoItem t = ortho_item<kWidth>(p, q);
+            bool ok = ptx::mbar_wait(ptx::smem_addr(&ctl->stored[n % kItems]), (n / kItems) & 1u, abort_flag, status_word);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            if (lane == 0) {
+                asm volatile("fence.proxy.async;\n\tfence.acq_rel.gpu;" ::: "memory");
+                asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.done + t.matrix) : "memory");
+                ptx::mbar_arrive(ptx::smem_addr(&ctl->item_empty[n % kItems]));
+            }
             __syncwarp();
-            if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&ctl->acc_empty[used & 1u]));
-            ++used;
-        };
-        for (uint32_t q = blockIdx.x; q < total; q += gridDim.x) {
-            const OrthoTile t = ortho_tile<kMode>(p, q, per);
-            float sum[kExact ? kTile : 1];
-            uint32_t taddr = 0;
+        }
+    } else if (warp >= kFirstEpilogueWarp) {
+        // the accumulator's rows 32 (warp % 4) .. + 31, kCols of its columns
+        OrthoWarp w;
+        w.ctl = ctl;
+        w.staging = smem_raw + (ring - raw) + kRing + kControl + (warp - kFirstEpilogueWarp) * (kStagingBytes / kEpilogueWarps);
+        w.abort_flag = abort_flag;
+        w.lane = lane;
+        w.quad = warp & 3;
+        w.half = (warp - kFirstEpilogueWarp) >> 2;
+        w.tmem = tmem + ((uint32_t)(w.quad * 32) << 16);
+        for (uint32_t n = 0;; ++n) {
+            uint32_t q;
+            if (!next_item(n, q) || q >= total) break;
+            const OrthoItem t = ortho_item<kWidth>(p, q);
+            bool ok;
             if constexpr (kExact) {
-#pragma unroll
-                for (int i = 0; i < kTile; ++i) sum[i] = 0.f;
-                const int parts = 1 + (p.blocks + kPartBlocks - 1) / kPartBlocks;
-                for (int part = 0; part < parts; ++part) {
-                    take(taddr);
-                    if (!ok) break;
-#pragma unroll
-                    for (int c = 0; c < kTile; c += 32) {
-                        float v[32];
-                        ptx::tmem_ld_32x32(taddr + c, v);
-                        ptx::tmem_ld_wait();
-#pragma unroll
-                        for (int i = 0; i < 32; ++i) sum[c + i] += v[i];
-                    }
-                    give_back();
-                }
+                ok = t.mode == kGram   ? ortho_epilogue_exact<kGram>(p, t, w)
+                     : t.mode == kPoly ? ortho_epilogue_exact<kPoly>(p, t, w)
+                                       : ortho_epilogue_exact<kStep>(p, t, w);
             } else {
-                take(taddr);
+                ok = t.mode == kGram   ? ortho_epilogue<kGram, kWidth, kCols>(p, t, w)
+                     : t.mode == kPoly ? ortho_epilogue<kPoly, kWidth, kCols>(p, t, w)
+                                       : ortho_epilogue<kStep, kWidth, kCols>(p, t, w);
             }
             if (!ok) break;
-            const int row0 = t.i * kTile + warp * 32, col0 = t.j * kTile;
-            const int rows = kSymmetric ? p.m : p.rows, ld = kSymmetric ? p.ldm : p.ldx;
-            __half* S = p.S + (int64_t)t.matrix * p.s_plane;         // (first numbers of A)
-            const int64_t s_all = (int64_t)p.count * p.s_plane, x_all = (int64_t)p.count * p.x_plane;
-#pragma unroll
-            for (int c0 = 0; c0 < kTile; c0 += 64) {
-                // a lane has one row of the accumulator: through shared memory into rows of eight lanes
-                if constexpr (kExact) {
-#pragma unroll
-                    for (int g = 0; g < 16; ++g)
-                        *reinterpret_cast<float4*>(staging + lane * 256 + ((g ^ (lane & 7)) << 4)) =
-                            make_float4(sum[c0 + 4 * g], sum[c0 + 4 * g + 1], sum[c0 + 4 * g + 2], sum[c0 + 4 * g + 3]);
-                } else {
-                    float va[32], vb[32];
-                    ptx::tmem_ld_32x32(taddr + c0, va);
-                    ptx::tmem_ld_32x32(taddr + c0 + 32, vb);
-                    ptx::tmem_ld_wait();
-#pragma unroll
-                    for (int g = 0; g < 8; ++g) {
-                        *reinterpret_cast<float4*>(staging + lane * 256 + ((g ^ (lane & 7)) << 4)) =
-                            make_float4(va[4 * g], va[4 * g + 1], va[4 * g + 2], va[4 * g + 3]);
-                        *reinterpret_cast<float4*>(staging + lane * 256 + (((g + 8) ^ (lane & 7)) << 4)) =
-                            make_float4(vb[4 * g], vb[4 * g + 1], vb[4 * g + 2], vb[4 * g + 3]);
-                    }
-                    if (c0 + 64 == kTile) give_back();
-                }
-                __syncwarp();
-                const int col = col0 + c0 + ch * 8;
-#pragma unroll 2
-                for (int i = 0; i < 8; ++i) {
-                    const int r = i * 4 + sub, row = row0 + r;
-                    float v[8];
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        const float4 f = *reinterpret_cast<const float4*>(staging + r * 256 + (((2 * ch + h) ^ (r & 7)) << 4));
-                        v[4 * h] = f.x;
-                        v[4 * h + 1] = f.y;
-                        v[4 * h + 2] = f.z;
-                        v[4 * h + 3] = f.w;
-                    }
-                    const bool in = row < rows && col < ld;          // (columns between the matrix's and its pitch are written and never read)
-                    const int64_t at = (int64_t)row * ld + col;
-                    if constexpr (kMode == kGram) {
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            v[e] *= kDown;                           // 2^24 A as it comes, 2^12 A as it is held
-                            if (in && row == col + e) p.diag_a[(int64_t)t.matrix * p.ldm + row] = v[e] * kDown;
-                        }
-                    } else if constexpr (kMode == kPoly) {
-                        float first[8] = {}, second[8] = {};
-                        if (in) unpack_half(*reinterpret_cast<const uint4*>(S + at), first);
-                        if (kExact && in) unpack_half(*reinterpret_cast<const uint4*>(S + s_all + at), second);
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) {
-                            const float a2 = v[e] * (kDown * kDown);
-                            if (in && row == col + e) {
-                                // the diagonal in fp32: A_ii as its product left it, and (A^2)_ii with that in A_ii's place
-                                const float d = p.diag_a[(int64_t)t.matrix * p.ldm + row];
-                                const float h = first[e] * kDown, l = kExact ? second[e] * kDown : 0.f;
-                                p.diag_b[(int64_t)t.matrix * p.ldm + row] = kNsB * d + kNsC * (a2 + (d - h) * (d + h) - 2.f * h * l);
-                                v[e] = 0.f;
-                            } else {
-                                v[e] = fmaf(kNsB, first[e] + second[e], kNsC * a2 * kUp);
-                            }
-                        }
-                    } else {
-                        float first[8] = {}, second[8] = {};
-                        const __half* X = p.X + (int64_t)p.buffer * 2 * x_all + (int64_t)t.matrix * p.x_plane;
-                        if (in) {
-                            unpack_half(*reinterpret_cast<const uint4*>(X + at), first);
-                            unpack_half(*reinterpret_cast<const uint4*>(X + x_all + at), second);
-                        }
-                        const float* diag = p.diag_b + (int64_t)t.matrix * p.ldm;
-                        float f[8];
-                        if (p.tall) {
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) f[e] = in ? kNsA + diag[col + e] : 0.f;      // (ld and ldm are the same here)
-                        } else {
-                            const float d = in ? kNsA + diag[row] : 0.f;
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) f[e] = d;
-                        }
-#pragma unroll
-                        for (int e = 0; e < 8; ++e) v[e] = fmaf(f[e], second[e], fmaf(f[e], first[e], v[e] * kDown));
-                    }
-                    if constexpr (kMode == kStep) {
-                        if (p.out != nullptr) {
-                            if (row >= p.rows) continue;
-                            const int64_t o = ((int64_t)t.matrix * p.rows + row) * p.cols + col;
-                            const float k = p.scale * kDown;
-                            if (p.out_bf16) {
-                                __nv_bfloat16* out = static_cast<__nv_bfloat16*>(p.out) + o;
-                                if (p.cols % 8 == 0) {
-                                    if (col < p.cols) {
-                                        uint32_t w[4];
-#pragma unroll
-                                        for (int e = 0; e < 4; ++e) {
-                                            const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * e] * k, v[2 * e + 1] * k);
-                                            w[e] = *reinterpret_cast<const uint32_t*>(&b);
-                                        }
-                                        *reinterpret_cast<uint4*>(out) = make_uint4(w[0], w[1], w[2], w[3]);
-                                    }
-                                } else {
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e)
-                                        if (col + e < p.cols) out[e] = __float2bfloat16_rn(v[e] * k);
-                                }
-                            } else {
-                                float* out = static_cast<float*>(p.out) + o;
-                                if (p.cols % 4 == 0) {
-#pragma unroll
-                                    for (int e = 0; e < 8; e += 4)
-                                        if (col + e < p.cols)
-                                            *reinterpret_cast<float4*>(out + e) = make_float4(v[e] * k, v[e + 1] * k, v[e + 2] * k, v[e + 3] * k);
-                                } else {
-#pragma unroll
-                                    for (int e = 0; e < 8; ++e)
-                                        if (col + e < p.cols) out[e] = v[e] * k;
-                                }
-                            }
-                        } else if (in) {
-                            __half* X = p.X + (int64_t)(p.buffer ^ 1) * 2 * x_all + (int64_t)t.matrix * p.x_plane;
-                            *reinterpret_cast<uint4*>(X + at) = pack_half(v);
-                            *reinterpret_cast<uint4*>(X + x_all + at) = pack_half(v);
-                        }
-                    } else {
-                        __half* to = S + (kMode == kPoly ? p.s_planes * s_all : 0);
-                        const uint4 first = pack_half(v);
-                        uint4 second = make_uint4(0u, 0u, 0u, 0u);
-                        if constexpr (kExact) second = pack_half(v);
-                        if (in) {
-                            *reinterpret_cast<uint4*>(to + at) = first;
-                            if constexpr (kExact) *reinterpret_cast<uint4*>(to + s_all + at) = second;
-                        }
-                        if (t.i != t.j) {                            // the other way: 64 rows of 32, 16-byte pieces swizzled
-                            const uint32_t a[4] = {first.x, first.y, first.z, first.w}, b[4] = {second.x, second.y, second.z, second.w};
-                            uint8_t* m = mirror + (((r >> 3) ^ (ch & 3)) << 4) + (r & 7) * 2;
-#pragma unroll
-                            for (int e = 0; e < 8; ++e) {
-                                *reinterpret_cast<uint16_t*>(m + (ch * 8 + e) * 64) = (uint16_t)(a[e >> 1] >> (16 * (e & 1)));
-                                if constexpr (kExact)
-                                    *reinterpret_cast<uint16_t*>(m + kMirrorBytes + (ch * 8 + e) * 64) = (uint16_t)(b[e >> 1] >> (16 * (e & 1)));
-                            }
-                        }
-                    }
-                }
-                __syncwarp();
-                if constexpr (kSymmetric) {
-                    if (t.i != t.j) {
-                        __half* to = S + (kMode == kPoly ? p.s_planes * s_all : 0);
-#pragma unroll
-                        for (int i = 0; i < 8; ++i) {
-                            const int c = i * 8 + (lane >> 2), g = lane & 3;
-                            const int row = col0 + c0 + c, at_col = row0 + g * 8;
-                            const uint8_t* m = mirror + c * 64 + ((g ^ ((c >> 3) & 3)) << 4);
-                            if (row < p.m && at_col < p.ldm) {
-                                const int64_t at = (int64_t)row * p.ldm + at_col;
-                                *reinterpret_cast<uint4*>(to + at) = *reinterpret_cast<const uint4*>(m);
-                                if constexpr (kExact) *reinterpret_cast<uint4*>(to + s_all + at) = *reinterpret_cast<const uint4*>(m + kMirrorBytes);
-                            }
-                        }
-                        __syncwarp();
-                    }
-                }
-            }
+            __syncwarp();
+            if (lane == 0) ptx::mbar_arrive(ptx::smem_addr(&ctl->stored[n % kItems]));
         }
     }
     ptx::tc_fence_before_sync();
     __syncthreads();
-    if (warp == 5) {
+    if (warp == kProductWarp) {
         ptx::tc_fence_after_sync();
-        ptx::tmem_dealloc(tmem, 2 * kTile);
+        ptx::tmem_dealloc(tmem, kTmemCols);
     }
 }
 
@@ -475,6 +855,8 @@ struct StartParams {
     const float* G;
     float* momentum;                 // nullable
     double* partial;                 // [count][blocks]: sums of squares
+    uint32_t* drawn;                 // the products' counters, cleared here
+    int32_t* done;
     __half* X;
     int64_t x_plane, elements;       // of a matrix: with pitch, without
     int count, rows, cols, ldx, blocks, nesterov;
@@ -495,6 +877,10 @@ __global__ void __launch_bounds__(kStartThreads) ortho_norm_kernel(const StartPa
     pdl_wait();
     if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
     const int matrix = blockIdx.y;
+    if (blockIdx.x == 0 && threadIdx.x == 0) {
+        p.done[matrix] = 0;
+        if (matrix == 0) *p.drawn = 0u;
+    }
     const int64_t base = (int64_t)matrix * p.elements;
     double s = 0.0;
     auto one = [&](float g, float& mom) {
@@ -615,9 +1001,9 @@ bool plane_map(CUtensorMap* map, const __half* base, int64_t planes, int64_t row
 
 struct OrthoLayout {
     int64_t m, ldx, ldm, x_plane, s_plane;
-    int s_planes, start_blocks;
+    int s_planes, b_plane, start_blocks;
     bool exact;
-    size_t S, diag_a, diag_b, partial, bytes;        // offsets behind the planes of X
+    size_t S, diag_a, diag_b, partial, counters, bytes;      // offsets behind the planes of X
 };
 OrthoLayout ortho_layout(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols) {
     OrthoLayout l;
@@ -626,36 +1012,42 @@ OrthoLayout ortho_layout(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols
     l.ldx = (cols + 7) / 8 * 8;
     l.ldm = (l.m + 7) / 8 * 8;
     l.exact = dt == SBP_F32 || l.m <= kExactSide;
-    l.s_planes = l.exact ? 2 : 1;
+    l.s_planes = l.exact ? 4 : 3;
+    l.b_plane = l.exact ? 2 : 1;
     l.x_plane = rows * l.ldx;
     l.s_plane = l.m * l.ldm;
     const int64_t want = (rows * cols / 4 + 4 * kStartThreads - 1) / (4 * kStartThreads);
     l.start_blocks = (int)(want < 1 ? 1 : want < kStartBlocksMost ? want : kStartBlocksMost);
     l.S = up((size_t)(4 * count * l.x_plane) * 2);
-    l.diag_a = l.S + up((size_t)(2 * l.s_planes * count * l.s_plane) * 2);
+    l.diag_a = l.S + up((size_t)(l.s_planes * count * l.s_plane) * 2);
     l.diag_b = l.diag_a + up((size_t)(count * l.ldm) * 4);
     l.partial = l.diag_b + up((size_t)(count * l.ldm) * 4);
-    l.bytes = l.partial + up((size_t)count * l.start_blocks * 8);
+    l.counters = l.partial + up((size_t)count * l.start_blocks * 8);
+    l.bytes = l.counters + up((size_t)(count + 1) * 4);
     return l;
 }
 
-template <int kMode, bool kExact>
-cudaError_t launch_product(const CUtensorMap& a, const CUtensorMap& b, const OrthoParams& p, cudaStream_t stream) {
-    const cudaError_t e = opt_in_dynamic_smem<ortho_product_kernel<kMode, kExact>>((int)kOrthoSmem);
+template <bool kExact, int kWidth>
+cudaError_t launch_products(const CUtensorMap& x_rows, const CUtensorMap& x_across, const CUtensorMap& s_rows, OrthoParams& p, cudaStream_t stream) {
+    const cudaError_t e = opt_in_dynamic_smem<ortho_kernel<kExact, kWidth>>((int)kOrthoSmem);
     if (e != cudaSuccess) return e;
-    const int64_t per = kMode == kStep ? (int64_t)p.tiles_i * p.tiles_j : (int64_t)p.tiles_i * (p.tiles_i + 1) / 2, total = per * p.count;
-    return launch_pdl(ortho_product_kernel<kMode, kExact>, dim3((unsigned)(total < kNumSMs ? total : kNumSMs)), dim3(kOrthoThreads), kOrthoSmem,
-                      stream, a, b, p);
+    const uint32_t tiles = (uint32_t)((p.m + kTile - 1) / kTile), wide = (uint32_t)((p.m + kWidth - 1) / kWidth);
+    p.sym_tiles = kWidth / kTile * wide * (wide + 1) / 2 - (kWidth / kTile * wide - tiles);
+    p.step_cols = (uint32_t)((p.cols + kWidth - 1) / kWidth);
+    p.step_tiles = (uint32_t)((p.rows + kTile - 1) / kTile) * p.step_cols;
+    const int64_t most = (int64_t)p.count * (p.step_tiles > p.sym_tiles ? p.step_tiles : p.sym_tiles);
+    return launch_pdl(ortho_kernel<kExact, kWidth>, dim3((unsigned)(most < kNumSMs ? most : kNumSMs)), dim3(ortho_threads(kExact)), kOrthoSmem, stream,
+                      x_rows, x_across, s_rows, p);
 }
 
 }  // namespace
 
 size_t orthogonalize_workspace_bytes(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols) { return ortho_layout(dt, count, rows, cols).bytes; }
 
-// the tiles of a launch, and the planes a tensor map counts, are 32-bit numbers
+// the items of a launch (three products of at most this many tiles, up to 32 times) and the planes a tensor map counts are 32-bit numbers
 bool orthogonalize_supported(int64_t count, int64_t rows, int64_t cols) {
     const int64_t tiles = (rows + kTile - 1) / kTile * ((cols + kTile - 1) / kTile);
-    return rows <= (1 << 16) && cols <= (1 << 16) && count <= (1 << 16) - 1 && tiles * count < (1ll << 30);
+    return rows <= (1 << 16) && cols <= (1 << 16) && count <= (1 << 16) - 1 && 3 * 32 * tiles * count < (1ll << 31);
 }
 
 cudaError_t launch_orthogonalize(sbp_dtype dt, const float* G, float* momentum, float beta, bool nesterov, int64_t count, int64_t rows, int64_t cols,
@@ -667,6 +1059,8 @@ cudaError_t launch_orthogonalize(sbp_dtype dt, const float* G, float* momentum, 
     s.momentum = momentum;
     s.partial = reinterpret_cast<double*>(ws + l.partial);
     s.X = reinterpret_cast<__half*>(ws);
+    s.drawn = reinterpret_cast<uint32_t*>(ws + l.counters);
+    s.done = reinterpret_cast<int32_t*>(ws + l.counters) + 1;
     s.x_plane = l.x_plane;
     s.elements = rows * cols;
     s.count = (int)count;
@@ -697,34 +1091,24 @@ cudaError_t launch_orthogonalize(sbp_dtype dt, const float* G, float* momentum, 
     p.m = (int)l.m;
     p.ldx = (int)l.ldx;
     p.ldm = (int)l.ldm;
-    p.s_planes = l.s_planes;
+    p.b_plane = l.b_plane;
     p.tall = rows > cols;
     p.out_bf16 = dt == SBP_BF16;
     p.scale = scale;
     p.status_word = status_word;
     CUtensorMap x_rows, x_across, s_rows;
     if (!plane_map(&x_rows, p.X, 4 * count, rows, cols, l.ldx, kTile) || !plane_map(&x_across, p.X, 4 * count, rows, cols, l.ldx, 64) ||
-        !plane_map(&s_rows, p.S, 2 * l.s_planes * count, l.m, l.m, l.ldm, kTile))
+        !plane_map(&s_rows, p.S, l.s_planes * count, l.m, l.m, l.ldm, kTile))
         return cudaErrorUnknown;
-    const CUtensorMap& gram = p.tall ? x_across : x_rows;
-    const int tiles_m = (int)((l.m + kTile - 1) / kTile);
-    for (int step = 0; step < steps; ++step) {
-        p.buffer = step & 1;
-        p.tiles_i = p.tiles_j = tiles_m;
-        p.blocks = (int)(((p.tall ? rows : cols) + kDeep - 1) / kDeep);
-        e = l.exact ? launch_product<kGram, true>(gram, gram, p, stream) : launch_product<kGram, false>(gram, gram, p, stream);
-        if (e != cudaSuccess) return e;
-        p.blocks = (int)((l.m + kDeep - 1) / kDeep);
-        e = l.exact ? launch_product<kPoly, true>(s_rows, s_rows, p, stream) : launch_product<kPoly, false>(s_rows, s_rows, p, stream);
-        if (e != cudaSuccess) return e;
-        p.tiles_i = (int)((rows + kTile - 1) / kTile);
-        p.tiles_j = (int)((cols + kTile - 1) / kTile);
-        p.out = step == steps - 1 ? O : nullptr;
-        const CUtensorMap &a = p.tall ? x_rows : s_rows, &b = p.tall ? s_rows : x_across;
-        e = l.exact ? launch_product<kStep, true>(a, b, p, stream) : launch_product<kStep, false>(a, b, p, stream);
-        if (e != cudaSuccess) return e;
-    }
-    return cudaSuccess;
+    p.gram_blocks = (int)(((p.tall ? rows : cols) + kDeep - 1) / kDeep);
+    p.m_blocks = (int)((l.m + kDeep - 1) / kDeep);
+    p.steps = steps;
+    p.out = O;
+    p.drawn = s.drawn;
+    p.done = s.done;
+    if (l.exact) return launch_products<true, 128>(x_rows, x_across, s_rows, p, stream);
+    return (rows + kTile - 1) / kTile * ((cols + kTile - 1) / kTile) * count > kNumSMs ? launch_products<false, 256>(x_rows, x_across, s_rows, p, stream)
+                                                                                       : launch_products<false, 128>(x_rows, x_across, s_rows, p, stream);
 }
 
 }  // namespace sbp
