@@ -23,9 +23,12 @@
 // the next.  (One launch a product, seventeen a call, cost 8 us each before their first tile.)  Operands come by TMA, X in either
 // orientation as it lies; tcgen05.mma into accumulators in turns; the epilogue forms the next operand from the sums.  A and B
 // are symmetric: only tiles on and above the diagonal are made, and stored both ways.
+#include "row_math.cuh"
 #include "tc_ptx.cuh"
 
 #include <cuda_fp16.h>
+
+#include <type_traits>
 
 namespace sbp {
 namespace {
@@ -847,6 +850,14 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
     }
 }
 
+// 2^12 / norm as a power of two and a number near 2^12, each of which fp32 holds
+__device__ __forceinline__ void inverse_norm(double norm, float& power, float& factor) {
+    int e = norm > 0.0 && isfinite(norm) ? ilogb(norm) : 0;
+    e = e > 126 ? 126 : e < -126 ? -126 : e;
+    power = scalbnf(1.f, -e);
+    factor = (float)(4096.0 / ldexp(norm, -e));
+}
+
 // ---- the start: momentum, the norm, the two fp16 numbers of U / (|U| + eps) ----
 constexpr int kStartThreads = 256;
 constexpr int kStartBlocksMost = 64;                                 // blocks a matrix
@@ -932,10 +943,8 @@ __global__ void __launch_bounds__(kStartThreads) ortho_scale_kernel(const StartP
     double s = 0.0;
     for (int b = 0; b < p.blocks; ++b) s += p.partial[(int64_t)matrix * p.blocks + b];
     const double norm = sqrt(s) + p.eps;
-    // 2^12 / norm as a power of two and a number near 2^12, each of which fp32 holds
-    int e = norm > 0.0 && isfinite(norm) ? ilogb(norm) : 0;
-    e = e > 126 ? 126 : e < -126 ? -126 : e;
-    const float power = scalbnf(1.f, -e), factor = (float)(4096.0 / ldexp(norm, -e));
+    float power, factor;
+    inverse_norm(norm, power, factor);
     const int64_t groups = (int64_t)p.rows * (p.ldx / 8);
     const float* G = p.G + (int64_t)matrix * p.elements;
     const float* mom = p.momentum != nullptr ? p.momentum + (int64_t)matrix * p.elements : nullptr;
@@ -972,6 +981,393 @@ __global__ void __launch_bounds__(kStartThreads) ortho_scale_kernel(const StartP
         for (int h = 0; h < 8; ++h) v[h] = v[h] * power * factor;
         *reinterpret_cast<uint4*>(X + (int64_t)row * p.ldx + col) = pack_half(v);
         *reinterpret_cast<uint4*>(X + second + (int64_t)row * p.ldx + col) = pack_half(v);
+    }
+}
+
+// ---- matrices with a side of at most 128: one launch, X in shared memory ----
+// A matrix with m = min(rows, cols) <= 128 is a cluster of up to eight blocks, each with a slice of at most 256 of the longer side's
+// positions in its shared memory for the whole call: as [128, slice] in 64 wide blocks of 128-byte rows, which are the
+// reduction-major operand of A and, unchanged, the other operand of B X (a tall matrix is turned when it is read).  A's partial
+// sums over the slices go to the blocks that own their rows, and A comes back to all of them, through distributed shared memory;
+// everything else stays in the block.  Momentum and norm included, it is one launch without a wait on another cluster.
+// Both fp16 numbers of every operand, as the other exact products; no chain of products is longer than four blocks here.
+constexpr int kSmallSide = 128, kSmallSlice = 256, kSmallCluster = 8, kSmallThreads = 512;
+constexpr uint32_t kSmallBlock = 128 * kRow;                        // 128 x 64 numbers
+constexpr uint32_t kSmallX = 4 * kSmallBlock, kSmallS = 2 * kSmallBlock;         // a plane of X, of A and B
+constexpr uint32_t kSmallSmem = 2 * kSmallX + 2 * kSmallS + 1024;
+static_assert(kSmallS * 2 == 128 * 128 * 4, "the partial sums of the rows a block owns take the place of A");
+
+struct SmallParams {
+    const float* G;
+    float* momentum;
+    void* out;
+    int rows, cols, m, n, slice, tall, steps, nesterov, out_bf16;
+    float beta, scale;
+    double eps;
+    int32_t* status_word;
+};
+
+__device__ __forceinline__ void st_cluster(uint32_t addr, float4 v) {
+    asm volatile("st.shared::cluster.v4.f32 [%0], {%1, %2, %3, %4};" ::"r"(addr), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, uint2 v) {
+    asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(addr), "r"(v.x), "r"(v.y) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, float v) {
+    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(addr), "f"(v) : "memory");
+}
+__device__ __forceinline__ void st_cluster(uint32_t addr, double v) {
+    asm volatile("st.shared::cluster.f64 [%0], %1;" ::"r"(addr), "d"(v) : "memory");
+}
+// byte offset of numbers (row, col .. ) of a [128, 64 k] plane: 64 wide blocks, 128-byte rows, 16-byte pieces swizzled
+__device__ __forceinline__ uint32_t small_at(int row, int col) {
+    return (uint32_t)(col >> 6) * kSmallBlock + (uint32_t)row * kRow + ((((uint32_t)col >> 3 & 7u) ^ ((uint32_t)row & 7u)) << 4) + ((uint32_t)col & 7u) * 2;
+}
+__global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const SmallParams p) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t product_done;
+    __shared__ uint32_t tmem_slot;
+    __shared__ int abort_slot;
+    __shared__ double warp_squares[kSmallThreads / 32], block_squares[kSmallCluster];
+    __shared__ float diag_a[kSmallSide], diag_b[kSmallSide];
+    const int warp = __shfl_sync(0xffffffffu, (int)(threadIdx.x >> 5), 0), lane = threadIdx.x & 31, tid = threadIdx.x;
+    uint32_t blocks, rank = ptx::cluster_ctarank();
+    asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(blocks));
+    const int matrix = blockIdx.x / blocks;
+    const uint32_t raw = ptx::smem_addr(smem_raw), base = (raw + 1023u) & ~1023u;
+    uint8_t* X = smem_raw + (base - raw);                           // first numbers, second numbers
+    uint8_t* S = X + 2 * kSmallX;
+    const uint32_t x_addr = base, s_addr = base + 2 * kSmallX;
+
+    pdl_launch_dependents();
+    if (tid == 0) {
+        ptx::mbar_init(ptx::smem_addr(&product_done), 1);
+        abort_slot = 0;
+        ptx::fence_mbar_init();
+    }
+    if (warp == 0) ptx::tmem_alloc(ptx::smem_addr(&tmem_slot), 512);
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    for (uint32_t i = tid; i < 2 * kSmallX / 16; i += kSmallThreads) reinterpret_cast<uint4*>(X)[i] = zero;
+    ptx::tc_fence_before_sync();
+    __syncthreads();
+    ptx::tc_fence_after_sync();
+    const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
+    volatile int* abort_flag = &abort_slot;
+    pdl_wait();
+    // (an error that lies before this call is seen by all blocks of the cluster alike, or by none that matter: a block that goes on
+    // alone would wait for the others, so they agree below)
+    const bool skip = p.status_word != nullptr && *reinterpret_cast<volatile int32_t*>(p.status_word) != 0;
+    bool ok = !skip;
+
+    // ---- momentum, norm, X ----
+    const int64_t elements = (int64_t)p.rows * p.cols;
+    const float* G = p.G + matrix * elements;
+    float* mom = p.momentum != nullptr ? p.momentum + matrix * elements : nullptr;
+    const int j0 = (int)rank * p.slice, width = p.n - j0 < p.slice ? p.n - j0 : p.slice;        // this block's positions (none: <= 0)
+    // numbers of G in groups along its rows (outer, inner ..): of four where they are aligned
+    const int outers = p.tall ? width : p.m, inners = p.tall ? p.m : width;
+    auto place = [&](int outer, int inner) { return p.tall ? (int64_t)(j0 + outer) * p.cols + inner : (int64_t)outer * p.cols + j0 + inner; };
+    auto visit_by = [&](auto size, auto f) {                         // f(u[], mo[]: gradient, momentum; outer, inner)
+        constexpr int N = decltype(size)::value;
+        // a warp has every sixteenth row, a lane every 32nd group; kBatch of them are loaded before any is stored
+        constexpr int kBatch = N == 4 ? 4 : 12;
+        const int groups = inners / N, chunks = (groups + 31) / 32;
+        int o = warp, c = 0;
+        while (o < outers && chunks > 0) {
+            float u[kBatch][N], mo[kBatch][N];
+            int outer[kBatch], inner[kBatch];
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i) {
+                const int g = c * 32 + lane;
+                outer[i] = o < outers && g < groups ? o : -1;
+                inner[i] = g * N;
+                if (++c == chunks) {
+                    c = 0;
+                    o += kSmallThreads / 32;
+                }
+#pragma unroll
+                for (int e = 0; e < N; ++e) u[i][e] = mo[i][e] = 0.f;
+                if (outer[i] < 0) continue;
+                const int64_t at = place(outer[i], inner[i]);
+                if constexpr (N == 4) {
+                    const float4 a = __ldg(reinterpret_cast<const float4*>(G + at));
+                    u[i][0] = a.x, u[i][1] = a.y, u[i][2] = a.z, u[i][3] = a.w;
+                    if (mom != nullptr) {
+                        const float4 b = *reinterpret_cast<const float4*>(mom + at);
+                        mo[i][0] = b.x, mo[i][1] = b.y, mo[i][2] = b.z, mo[i][3] = b.w;
+                    }
+                } else {
+                    u[i][0] = __ldg(G + at);
+                    if (mom != nullptr) mo[i][0] = mom[at];
+                }
+            }
+#pragma unroll
+            for (int i = 0; i < kBatch; ++i)
+                if (outer[i] >= 0) f(u[i], mo[i], outer[i], inner[i]);
+        }
+    };
+    auto visit = [&](auto f) {                                       // (where cols is a multiple of four, so is every block's share)
+        if (p.cols % 4 == 0) visit_by(std::integral_constant<int, 4>(), f);
+        else visit_by(std::integral_constant<int, 1>(), f);
+    };
+    double squares = 0.0;
+    if (ok) {
+        visit([&](auto& u, auto& mo, int outer, int inner) {
+            constexpr int N = sizeof(u) / sizeof(float);
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+                if (mom != nullptr) {
+                    mo[e] = fmaf(p.beta, mo[e], u[e]);
+                    u[e] = p.nesterov ? fmaf(p.beta, mo[e], u[e]) : mo[e];
+                }
+                squares = fma((double)u[e], (double)u[e], squares);
+            }
+            if (mom == nullptr) return;
+            const int64_t at = place(outer, inner);
+            if constexpr (N == 4) *reinterpret_cast<float4*>(mom + at) = make_float4(mo[0], mo[1], mo[2], mo[3]);
+            else mom[at] = mo[0];
+        });
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) squares += __shfl_xor_sync(0xffffffffu, squares, o);
+    if (lane == 0) warp_squares[warp] = squares;
+    ptx::cluster_sync_all();                                         // (a barrier of the block, and every block has begun)
+    if (tid < (int)blocks) {
+        double s = 0.0;
+        for (int w = 0; w < kSmallThreads / 32; ++w) s += warp_squares[w];
+        if (skip) s = -1.0;
+        st_cluster(ptx::map_to_cta(ptx::smem_addr(&block_squares[rank]), (uint32_t)tid), s);
+    }
+    ptx::cluster_sync_all();
+    {
+        double s = 0.0;
+        for (uint32_t b = 0; b < blocks; ++b) {
+            s += block_squares[b];
+            if (block_squares[b] < 0.0) ok = false;                  // some block has seen an error: none goes on
+        }
+        float power, factor;
+        inverse_norm(sqrt(s) + p.eps, power, factor);
+        if (ok) {
+            visit([&](auto& u, auto& mo, int outer, int inner) {
+                constexpr int N = sizeof(u) / sizeof(float);
+#pragma unroll
+                for (int e = 0; e < N; ++e) {
+                    if (mom != nullptr) u[e] = p.nesterov ? fmaf(p.beta, mo[e], u[e]) : mo[e];
+                    const float x = u[e] * power * factor;
+                    const uint32_t at = p.tall ? small_at(inner + e, outer) : small_at(outer, inner + e);
+                    const __half h = __float2half_rn(x);
+                    *reinterpret_cast<__half*>(X + at) = h;
+                    *reinterpret_cast<__half*>(X + kSmallX + at) = __float2half_rn(x - __half2float(h));
+                }
+            });
+        }
+    }
+
+    // ---- the steps ----
+    const int quad = warp & 3, row = quad * 32 + lane, cols0 = (warp >> 2) * 32;       // epilogues: a lane's row, a warp's columns
+    const uint32_t lane_tmem = tmem + ((uint32_t)(quad * 32) << 16);
+    // tensor memory: A and its polynomial in columns 0 .. 127, the next X in 256 ..; the small products of the three, first x second
+    // and second x first, 128 columns further on (an instruction that adds to the place of the one before it waits for it),
+    // where a slice of over 128 positions does not need them
+    const bool narrow = p.slice <= 128;
+    const uint32_t d_sym = 0, d_step = 256;
+    const int m16 = (p.m + 15) / 16 * 16, deep_m = (p.m + kDeep - 1) / kDeep, deep_n = p.slice / kDeep;
+    uint32_t phase = 0;
+    // products of a and b (reduction along their rows, or down b's: across), the small ones to `two` where that is another place
+    auto multiply = [&](uint32_t d, uint32_t two, uint32_t a, uint32_t a_plane, uint32_t b, uint32_t b_plane, bool across, int width_n, int blocks_k) {
+        asm volatile("fence.proxy.async;" ::: "memory");             // what this thread wrote to shared memory, for the tensor core
+        ptx::tc_fence_before_sync();
+        __syncthreads();
+        if (warp == 0 && ok) {
+            ptx::tc_fence_after_sync();
+            const bool leader = ptx::elect_one();
+            const uint32_t idesc = ptx::umma_idesc_f16(kTile, width_n, false, across);
+            const uint32_t a_lo = ptx::umma_desc_lo(a, 16u), b_lo = ptx::umma_desc_lo(b, across ? kSmallBlock : 16u);
+#pragma unroll 1
+            for (int k = 0; k < blocks_k; ++k)
+#pragma unroll
+                for (uint32_t u = 0; u < kDeep / kUmmaDeep; ++u) {
+                    // along: 32 bytes of a row, the next 64 in the next block; across: 16 rows down, 64 rows in a deep block
+                    const uint32_t au = a_lo + ((k * kSmallBlock + u * kUmmaDeep * 2) >> 4);
+                    const uint32_t bu = b_lo + ((across ? k * kHalfOperand + u * kUmmaDeep * kRow : k * kSmallBlock + u * kUmmaDeep * 2) >> 4);
+                    const bool more = k != 0 || u != 0u;
+                    ptx::umma_bf16_warp<false>(tmem + two, ptx::umma_desc_of(au + (a_plane >> 4)), ptx::umma_desc_of(bu), idesc, more, leader);
+                    ptx::umma_bf16_warp<false>(tmem + d, ptx::umma_desc_of(au), ptx::umma_desc_of(bu), idesc, more || two == d, leader);
+                    ptx::umma_bf16_warp<false>(tmem + two, ptx::umma_desc_of(au), ptx::umma_desc_of(bu + (b_plane >> 4)), idesc, true, leader);
+                }
+            if (leader) ptx::umma_commit(ptx::smem_addr(&product_done));
+            __syncwarp();
+        }
+        if (ok) ok = ptx::mbar_wait(ptx::smem_addr(&product_done), phase & 1u, abort_flag, p.status_word);
+        ok = __all_sync(0xffffffffu, ok);
+        ++phase;
+        ptx::tc_fence_after_sync();
+    };
+    auto sums = [&](uint32_t d, uint32_t two, float (&v)[32]) {      // of this lane's row, 32 columns from d on
+        ptx::tmem_ld_32x32(lane_tmem + d, v);
+        if (two != d) {
+            float w[32];
+            ptx::tmem_ld_32x32(lane_tmem + two, w);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 32; ++e) v[e] += w[e];
+        } else {
+            ptx::tmem_ld_wait();
+        }
+    };
+    // 32 numbers of a row, times 2^12, as two fp16 numbers each
+    auto put = [&](uint8_t* plane, uint32_t second, int r, int c, float (&v)[32]) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint32_t at = small_at(r, c + 8 * g);
+            *reinterpret_cast<uint4*>(plane + at) = pack_half(&v[8 * g]);
+            *reinterpret_cast<uint4*>(plane + second + at) = pack_half(&v[8 * g]);
+        }
+    };
+    for (int step = 0; step < p.steps; ++step) {
+        // A: every block's share of the sum
+        multiply(d_sym, d_sym + 128, x_addr, kSmallX, x_addr, kSmallX, false, m16, deep_n);
+        float v[32];
+        sums(d_sym + cols0, d_sym + 128 + cols0, v);
+#pragma unroll
+        for (int e = 0; e < 32; ++e) v[e] = cols0 + e < m16 ? v[e] * kDown : 0.f;      // (columns that no product wrote)
+        if (blocks == 1) {
+#pragma unroll
+            for (int e = 0; e < 32; ++e)
+                if (cols0 + e == row) diag_a[row] = v[e] * kDown;
+            put(S, kSmallS, row, cols0, v);
+        } else {
+            const int own = kSmallSide / (int)blocks;                // rows a block owns
+            // the partial rows go where X has no positions, or else to the place of A and B, once no block reads them any more
+            auto partial = [&](int r) { return narrow ? (uint32_t)(r < 64 ? 0 : kSmallX) + kSmallX / 2 + (uint32_t)(r & 63) * 512 : 2 * kSmallX + (uint32_t)r * 512; };
+            const uint32_t to = ptx::map_to_cta(x_addr, (uint32_t)(row / own)) + partial((int)rank * own + row % own);
+            if (step > 0 && !narrow) asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");        // no block reads its A or B any more
+#pragma unroll
+            for (int g = 0; g < 8; ++g)
+                st_cluster(to + (((uint32_t)(cols0 / 4 + g) ^ ((uint32_t)row & 7u)) << 4), make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]));
+            ptx::cluster_sync_all();
+            float4 a[4];
+            const int items = own * 32;                              // (row, four columns) of the owned rows
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int item = tid + i * kSmallThreads;
+                a[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+                if (item >= items) continue;
+                const int r = item >> 5;
+                for (uint32_t b = 0; b < blocks; ++b) {              // (own is a multiple of eight: the swizzle is the row's)
+                    const float4 q = *reinterpret_cast<const float4*>(X + partial((int)b * own + r) + (((item & 31) ^ (r & 7)) << 4));
+                    a[i].x += q.x;
+                    a[i].y += q.y;
+                    a[i].z += q.z;
+                    a[i].w += q.w;
+                }
+            }
+            if (!narrow) ptx::cluster_sync_all();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const int item = tid + i * kSmallThreads;
+                if (item >= items) continue;
+                const int r = (int)rank * own + (item >> 5), c = (item & 31) * 4;
+                const float q[4] = {a[i].x, a[i].y, a[i].z, a[i].w};
+                __half2 h[2], l[2];
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    h[e] = __floats2half2_rn(q[2 * e], q[2 * e + 1]);
+                    const float2 f = __half22float2(h[e]);
+                    l[e] = __floats2half2_rn(q[2 * e] - f.x, q[2 * e + 1] - f.y);
+                }
+                const uint2 first = make_uint2(*reinterpret_cast<uint32_t*>(&h[0]), *reinterpret_cast<uint32_t*>(&h[1]));
+                const uint2 second = make_uint2(*reinterpret_cast<uint32_t*>(&l[0]), *reinterpret_cast<uint32_t*>(&l[1]));
+                float diagonal = 0.f;
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+                    if (c + e == r) diagonal = q[e] * kDown;
+                for (uint32_t b = 0; b < blocks; ++b) {
+                    const uint32_t at = ptx::map_to_cta(s_addr + small_at(r, c), b);
+                    st_cluster(at, first);
+                    st_cluster(at + kSmallS, second);
+                    if (r >= c && r < c + 4) st_cluster(ptx::map_to_cta(ptx::smem_addr(&diag_a[r]), b), diagonal);
+                }
+            }
+            ptx::cluster_sync_all();
+        }
+        // B = b A + c A^2, its diagonal apart in fp32
+        multiply(d_sym, d_sym + 128, s_addr, kSmallS, s_addr, kSmallS, false, m16, deep_m);
+        sums(d_sym + cols0, d_sym + 128 + cols0, v);
+        const float d = diag_a[row];
+        float on_diagonal = 0.f;
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const uint32_t at = small_at(row, cols0 + 8 * g);
+            float first[8], second[8];
+            unpack_half(*reinterpret_cast<const uint4*>(S + at), first);
+            unpack_half(*reinterpret_cast<const uint4*>(S + kSmallS + at), second);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float a2 = cols0 + 8 * g + e < m16 ? v[8 * g + e] * (kDown * kDown) : 0.f;
+                v[8 * g + e] = fmaf(kNsB, first[e] + second[e], kNsC * a2 * kUp);
+                if (cols0 == quad * 32) {                            // (the same in the whole warp)
+                    const float h = first[e] * kDown, l = second[e] * kDown, b = kNsB * d + kNsC * (a2 + (d - h) * (d + h) - 2.f * h * l);
+                    on_diagonal = 8 * g + e == lane ? b : on_diagonal;
+                    v[8 * g + e] = 8 * g + e == lane ? 0.f : v[8 * g + e];
+                }
+            }
+        }
+        if (cols0 == quad * 32) diag_b[row] = on_diagonal;
+        put(S, kSmallS, row, cols0, v);
+        // X <- a X + B X
+        const uint32_t d_two = narrow ? d_step + 128 : d_step;
+        multiply(d_step, d_two, s_addr, kSmallS, x_addr, kSmallX, true, p.slice, deep_m);
+        const float f = kNsA + diag_b[row];
+        const bool last = step == p.steps - 1;
+        if (blocks > 1 && !narrow && !last) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
+        for (int pass = 0; pass < p.slice; pass += 128) {
+            const int c0 = cols0 + pass;
+            if (c0 < p.slice) {                                      // (the same in the whole warp)
+                sums(d_step + c0, d_two + c0, v);
+#pragma unroll
+                for (int g = 0; g < 4; ++g) {
+                    const uint32_t at = small_at(row, c0 + 8 * g);
+                    float first[8], second[8];
+                    unpack_half(*reinterpret_cast<const uint4*>(X + at), first);
+                    unpack_half(*reinterpret_cast<const uint4*>(X + kSmallX + at), second);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) v[8 * g + e] = fmaf(f, second[e], fmaf(f, first[e], v[8 * g + e] * kDown));
+                }
+                if (!last) {
+                    put(X, kSmallX, row, c0, v);
+                } else {                                             // to the place of B: fp32 rows of 128, 16-byte pieces swizzled
+#pragma unroll
+                    for (int g = 0; g < 8; ++g)
+                        *reinterpret_cast<float4*>(S + row * 512 + (((cols0 / 4 + g) ^ (row & 7)) << 4)) =
+                            make_float4(v[4 * g], v[4 * g + 1], v[4 * g + 2], v[4 * g + 3]);
+                }
+            }
+            if (!last) continue;
+            __syncthreads();
+            const int have = width - pass < 128 ? width - pass : 128;
+            auto out = [&](int r, int c) {                           // consecutive lanes write consecutive numbers
+                const float x = *reinterpret_cast<const float*>(S + r * 512 + (((c >> 2) ^ (r & 7)) << 4) + (c & 3) * 4) * (p.scale * kDown);
+                const int64_t o = matrix * elements + (p.tall ? place(pass + c, r) : place(r, pass + c));
+                if (p.out_bf16) static_cast<__nv_bfloat16*>(p.out)[o] = __float2bfloat16_rn(x);
+                else static_cast<float*>(p.out)[o] = x;
+            };
+            if (ok && p.tall) {
+                for (int c = warp; c < have; c += kSmallThreads / 32)
+                    for (int r = lane; r < p.m; r += 32) out(r, c);
+            } else if (ok) {
+                for (int r = warp; r < p.m; r += kSmallThreads / 32)
+                    for (int c = lane; c < have; c += 32) out(r, c);
+            }
+            __syncthreads();
+        }
+        ptx::tc_fence_before_sync();
+    }
+    __syncthreads();
+    ptx::cluster_sync_all();                                         // no block leaves while another may write to it
+    if (warp == 0) {
+        ptx::tc_fence_after_sync();
+        ptx::tmem_dealloc(tmem, 512);
     }
 }
 
@@ -1040,9 +1436,46 @@ cudaError_t launch_products(const CUtensorMap& x_rows, const CUtensorMap& x_acro
                       x_rows, x_across, s_rows, p);
 }
 
+// Blocks of a matrix's cluster, and the positions of the longer side each has; 0 where the other kernels take the matrix.  A step is
+// 6.5 us without other blocks (128 positions; 10 with 256) and 12.4 with: 100 x 257, momentum included, 80 us on four blocks and 89
+// on two, 100 x 256 67 us on one and 71 on two.
+int ortho_small_blocks(int64_t n) { return n <= 256 ? 1 : n <= 512 ? 4 : 8; }
+int ortho_small_slice(int64_t rows, int64_t cols) {
+    const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
+    if (m > kSmallSide || n > kSmallCluster * kSmallSlice) return 0;
+    const int64_t blocks = ortho_small_blocks(n);
+    return (int)((n + blocks * kDeep - 1) / (blocks * kDeep) * kDeep);
+}
+cudaError_t launch_small(sbp_dtype dt, const float* G, float* momentum, float beta, bool nesterov, int64_t count, int64_t rows, int64_t cols, int steps,
+                         double eps, float scale, void* O, int32_t* status_word, cudaStream_t stream) {
+    const cudaError_t e = opt_in_dynamic_smem<ortho_small_kernel>((int)kSmallSmem);
+    if (e != cudaSuccess) return e;
+    SmallParams p = {};
+    p.G = G;
+    p.momentum = momentum;
+    p.out = O;
+    p.rows = (int)rows;
+    p.cols = (int)cols;
+    p.tall = rows > cols;
+    p.m = (int)(p.tall ? cols : rows);
+    p.n = (int)(p.tall ? rows : cols);
+    p.slice = ortho_small_slice(rows, cols);
+    p.steps = steps;
+    p.nesterov = nesterov;
+    p.out_bf16 = dt == SBP_BF16;
+    p.beta = beta;
+    p.scale = scale;
+    p.eps = eps;
+    p.status_word = status_word;
+    const unsigned blocks = (unsigned)ortho_small_blocks(p.n);
+    return launch_pdl_cluster(ortho_small_kernel, dim3((unsigned)count * blocks), dim3(kSmallThreads), kSmallSmem, blocks, stream, p);
+}
+
 }  // namespace
 
-size_t orthogonalize_workspace_bytes(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols) { return ortho_layout(dt, count, rows, cols).bytes; }
+size_t orthogonalize_workspace_bytes(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols) {
+    return ortho_small_slice(rows, cols) > 0 ? 256 : ortho_layout(dt, count, rows, cols).bytes;
+}
 
 // the items of a launch (three products of at most this many tiles, up to 32 times) and the planes a tensor map counts are 32-bit numbers
 bool orthogonalize_supported(int64_t count, int64_t rows, int64_t cols) {
@@ -1052,6 +1485,8 @@ bool orthogonalize_supported(int64_t count, int64_t rows, int64_t cols) {
 
 cudaError_t launch_orthogonalize(sbp_dtype dt, const float* G, float* momentum, float beta, bool nesterov, int64_t count, int64_t rows, int64_t cols,
                                  int steps, double eps, float scale, void* O, void* workspace, int32_t* status_word, cudaStream_t stream) {
+    if (ortho_small_slice(rows, cols) > 0)
+        return launch_small(dt, G, momentum, beta, nesterov, count, rows, cols, steps, eps, scale, O, status_word, stream);
     const OrthoLayout l = ortho_layout(dt, count, rows, cols);
     uint8_t* ws = static_cast<uint8_t*>(workspace);
     StartParams s = {};
