@@ -11,8 +11,11 @@
 // so its statistics are made again there instead of being kept.  Means and variances are taken in two steps (the mean first,
 // then the squares of what is left), since the one-step form loses the variance of rows whose mean is large against it.
 // All arithmetic is fp32; R is normalised before it is rounded.
+#include "row_copy.cuh"
 #include "row_math.cuh"
 #include "zero_rows.cuh"
+
+#include <type_traits>
 
 namespace sbp {
 namespace {
@@ -25,161 +28,185 @@ struct NormFwdParams {
     uint4 *R, *Z, *Y_keep, *R_keep, *Z_keep;
     const int32_t *keep_rows, *M_keep_dev, *status_word;
     int64_t M, M_keep_cap;
-    int64_t gate_group;
-    int vecs, warps, chunk;                           // 16-byte vectors of a row; warps that share a row; rows of a worker
+    FastDiv gate_group;
+    int vecs, chunk;                                  // 16-byte vectors of a row; rows of a warp (or block)
     float scale, eps, inv_c;
     int caches;
 };
 
-// A worker (a warp, or a block where a row is long) takes `chunk` <= 32 consecutive rows, kU at a time; a thread holds kNV vectors
-// of each.  Which of the rows are kept, and the place of each in the caches, comes from one search of the list a chunk.
-template <typename T, int kNV, int kU, bool kMulti, bool kLayer, bool kPost>
-__global__ void __launch_bounds__(kMulti ? 512 : 256, kMulti ? 1 : 2)
+// kLanes threads of a warp share a row (kLanes 0: a block, for long rows), each with kNV vectors of it, kU rows at a time; the rows of a
+// warp, `chunk` <= 32 consecutive ones, are dealt to its groups of lanes in turn.  Which of them are kept, and the place of each in
+// the caches, comes from one search of the list.  kFull: the threads' vectors are the row's, none lies behind it (what those
+// would hold stays zero otherwise, at the price of a branch a vector, across which nothing is scheduled).
+template <typename T, int kNV, int kLanes, bool kFull, bool kLayer, bool kPost>
+__global__ void __launch_bounds__(kNV * Vec<T>::N > 8 ? 512 : 256, kNV * Vec<T>::N > 8 ? 1 : 4)
 norm_forward_kernel(const NormFwdParams p) {
-    constexpr int VN = Vec<T>::N;
-    constexpr int E = kNV * VN;
-    __shared__ float scratch[kMulti ? 2 * 32 * kU : 1];
+    constexpr bool kMulti = kLanes == 0;
+    constexpr int VN = Vec<T>::N, P = VN / 2, E2 = kNV * P;          // pairs of a vector, pairs a thread holds of a row
+    constexpr int kU = E2 > 4 ? 1 : 2;
+    constexpr int kGroups = kMulti ? 1 : 32 / (kMulti ? 32 : kLanes);
+    __shared__ float4 scratch[kMulti ? 32 : 1];
     pdl_launch_dependents();
     pdl_wait();
     if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
     const int lane = threadIdx.x & 31;
     const int64_t worker = kMulti ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
     const int64_t workers = kMulti ? (int64_t)gridDim.x : (int64_t)gridDim.x * (blockDim.x >> 5);
-    const int t = kMulti ? (int)threadIdx.x : lane, threads = kMulti ? (int)blockDim.x : 32;
+    RowThreads<kLanes> row = {kMulti ? (int)threadIdx.x : lane % (kMulti ? 32 : kLanes), (int)blockDim.x, (int)blockDim.x >> 5, 1, 0, scratch};
+    const int group = kMulti ? 0 : lane / (kMulti ? 32 : kLanes), threads = row.threads();
     const int64_t M_keep = p.caches ? load_m_keep(p.M_keep_dev, p.M_keep_cap) : 0;
-    const int64_t lo = worker * p.chunk, hi = lo + p.chunk < p.M ? lo + p.chunk : p.M;
-    int turn = 0;
+    const int64_t lo = worker * p.chunk;
+    const int count = lo < p.M ? (p.M - lo < p.chunk ? (int)(p.M - lo) : p.chunk) : 0;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    bool in[kNV];
+#pragma unroll
+    for (int j = 0; j < kNV; ++j) in[j] = kFull || row.t + j * threads < p.vecs;
 
-    if (lo < hi) {
+    if (count > 0) {
         uint32_t kept = 0u;                           // bit d: row lo + d is in the list
         int64_t place = 0;                            // of the first of them
-        if (p.caches) {
-            if (p.keep_rows == nullptr) {
-                const int64_t n = M_keep - lo;
-                kept = n >= 32 ? 0xffffffffu : n > 0 ? (1u << n) - 1u : 0u;
-                place = lo;
-            } else {
-                place = warp_lower_bound(p.keep_rows, M_keep, lo, lane);
-                const int64_t d = place + lane < M_keep ? (int64_t)__ldg(p.keep_rows + place + lane) - lo : 32;
-                kept = __reduce_or_sync(0xffffffffu, d >= 0 && d < 32 ? 1u << d : 0u);
-            }
-        }
-        for (int64_t row0 = lo; row0 < hi; row0 += kU) {
-            float x[kU][E];
+        for (int d0 = 0; d0 < count; d0 += kU * kGroups) {
+            f32x2 x[kU][E2];
             uint4 yq[kU][kNV], hq[kU][kNV];
+            int64_t at[kU];
+            bool live[kU];
 #pragma unroll
-            for (int u = 0; u < kU; ++u)
+            for (int u = 0; u < kU; ++u) {
+                const int d = d0 + u * kGroups + group;
+                live[u] = d < count;
+                at[u] = (lo + d) * p.vecs + row.t;
 #pragma unroll
                 for (int j = 0; j < kNV; ++j) {
-                    const int v = t + j * threads;
-                    const bool in = v < p.vecs && row0 + u < hi;
-                    yq[u][j] = in && p.Y != nullptr ? ld_row(p.Y + (row0 + u) * p.vecs + v) : make_uint4(0u, 0u, 0u, 0u);
-                    hq[u][j] = in && p.H != nullptr ? ld_row(p.H + (row0 + u) * p.vecs + v) : make_uint4(0u, 0u, 0u, 0u);
+                    yq[u][j] = in[j] && live[u] && p.Y != nullptr ? __ldcg(p.Y + at[u] + j * threads) : zero;
+                    hq[u][j] = in[j] && live[u] && p.H != nullptr ? __ldcg(p.H + at[u] + j * threads) : zero;
                 }
+            }
+            if (d0 == 0 && p.caches) {                // (under the first rows' loads)
+                if (p.keep_rows == nullptr) {
+                    const int64_t n = M_keep - lo;
+                    kept = n >= 32 ? 0xffffffffu : n > 0 ? (1u << n) - 1u : 0u;
+                    place = lo;
+                } else {
+                    place = warp_lower_bound(p.keep_rows, M_keep, lo, lane);
+                    const int64_t d = place + lane < M_keep ? (int64_t)__ldg(p.keep_rows + place + lane) - lo : 32;
+                    kept = __reduce_or_sync(0xffffffffu, d >= 0 && d < 32 ? 1u << d : 0u);
+                }
+            }
 #pragma unroll
             for (int u = 0; u < kU; ++u)
 #pragma unroll
-                for (int j = 0; j < kNV; ++j) Vec<T>::unpack(yq[u][j], &x[u][j * VN]);
+                for (int j = 0; j < kNV; ++j) Vec<T>::unpack(yq[u][j], &x[u][j * P]);
             auto normalise = [&](const float* w, const float* b) {
                 float s[kU];
                 if constexpr (kLayer) {
 #pragma unroll
                     for (int u = 0; u < kU; ++u) {
-                        s[u] = 0.f;
+                        f32x2 a = x[u][0];
 #pragma unroll
-                        for (int e = 0; e < E; ++e) s[u] += x[u][e];
+                        for (int e = 1; e < E2; ++e) a = add(a, x[u][e]);
+                        s[u] = both(a).x + both(a).y;
                     }
-                    row_sums<kU, kMulti>(s, scratch, p.warps, turn);
+                    row.sums(s);
 #pragma unroll
                     for (int u = 0; u < kU; ++u)
 #pragma unroll
                         for (int j = 0; j < kNV; ++j) {
-                            const float mean = t + j * threads < p.vecs ? s[u] * p.inv_c : 0.f;     // threads past the row hold zeros
+                            const float m = in[j] ? -s[u] * p.inv_c : 0.f;          // threads past the row hold zeros
 #pragma unroll
-                            for (int e = 0; e < VN; ++e) x[u][j * VN + e] -= mean;
+                            for (int e = 0; e < P; ++e) x[u][j * P + e] = add(x[u][j * P + e], pair(m, m));
                         }
                 }
 #pragma unroll
                 for (int u = 0; u < kU; ++u) {
-                    s[u] = 0.f;
+                    f32x2 a = mul(x[u][0], x[u][0]);
 #pragma unroll
-                    for (int e = 0; e < E; ++e) s[u] = fmaf(x[u][e], x[u][e], s[u]);
+                    for (int e = 1; e < E2; ++e) a = fma(x[u][e], x[u][e], a);
+                    s[u] = both(a).x + both(a).y;
                 }
-                row_sums<kU, kMulti>(s, scratch, p.warps, turn);
+                row.sums(s);
 #pragma unroll
                 for (int u = 0; u < kU; ++u) s[u] = rsqrtf(fmaf(s[u], p.inv_c, p.eps));
 #pragma unroll
                 for (int j = 0; j < kNV; ++j) {
-                    const int v = t + j * threads;
-                    if (v >= p.vecs) continue;
-                    float wf[VN], bf[VN];
-                    load_f32<VN>(w + v * VN, wf);
-                    if (b != nullptr) load_f32<VN>(b + v * VN, bf);
+                    if (!in[j]) continue;
+                    f32x2 wf[P], bf[P];
+                    load_f32<VN>(w + (row.t + j * threads) * VN, wf);
+                    if (b != nullptr) {
+                        load_f32<VN>(b + (row.t + j * threads) * VN, bf);
+                    } else {
+#pragma unroll
+                        for (int e = 0; e < P; ++e) bf[e] = pair(-0.f, -0.f);
+                    }
 #pragma unroll
                     for (int u = 0; u < kU; ++u)
 #pragma unroll
-                        for (int e = 0; e < VN; ++e) {
-                            const float n = x[u][j * VN + e] * s[u];
-                            x[u][j * VN + e] = b != nullptr ? fmaf(n, wf[e], bf[e]) : n * wf[e];
-                        }
+                        for (int e = 0; e < P; ++e) x[u][j * P + e] = fma(mul(x[u][j * P + e], pair(s[u], s[u])), wf[e], bf[e]);
                 }
             };
             if constexpr (kPost) normalise(p.post_w, p.post_b);
+            int64_t slot[kU];
+            bool keep[kU];
 #pragma unroll
             for (int u = 0; u < kU; ++u) {
-                const int64_t row = row0 + u;
-                const bool live = row < hi;
-                const bool keep = live && (kept >> (int)(row - lo) & 1u);
-                const int64_t slot = place + __popc(kept & ((1u << (int)((row - lo) & 31)) - 1u));
-                const uint4* gate = p.gate != nullptr && live ? p.gate + row / p.gate_group * p.vecs : nullptr;
+                const int d = (d0 + u * kGroups + group) & 31;
+                keep[u] = live[u] && (kept >> d & 1u);
+                slot[u] = (place + __popc(kept & ((1u << d) - 1u))) * p.vecs + row.t;
+                if (p.gate != nullptr && live[u]) {
+                    const uint4* gate = p.gate + (int64_t)p.gate_group((uint32_t)(lo + d0 + u * kGroups + group)) * p.vecs + row.t;
+#pragma unroll
+                    for (int j = 0; j < kNV; ++j) {
+                        if (!in[j]) continue;
+                        f32x2 g[P];
+                        Vec<T>::unpack(__ldg(gate + j * threads), g);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) x[u][j * P + e] = mul(x[u][j * P + e], g[e]);
+                    }
+                }
+                uint4 r[kNV];
 #pragma unroll
                 for (int j = 0; j < kNV; ++j) {
-                    const int v = t + j * threads;
-                    if (v >= p.vecs || !live) continue;
-                    float h[VN];
+                    f32x2 h[P];
                     Vec<T>::unpack(hq[u][j], h);
-                    if (gate != nullptr) {
-                        float g[VN];
-                        Vec<T>::unpack(__ldg(gate + v), g);
 #pragma unroll
-                        for (int e = 0; e < VN; ++e) x[u][j * VN + e] *= g[e];
-                    }
-                    if (p.H != nullptr) {
+                    for (int e = 0; e < P; ++e) x[u][j * P + e] = p.H != nullptr ? fma(pair(p.scale, p.scale), h[e], x[u][j * P + e]) : x[u][j * P + e];
+                    r[j] = Vec<T>::pack(&x[u][j * P]);
+                }
+                if (p.R != nullptr && live[u]) {
 #pragma unroll
-                        for (int e = 0; e < VN; ++e) x[u][j * VN + e] = fmaf(p.scale, h[e], x[u][j * VN + e]);
-                    }
-                    const uint4 r = Vec<T>::pack(&x[u][j * VN]);
-                    if (p.R != nullptr) p.R[row * p.vecs + v] = r;
-                    if (keep) {
-                        if (p.R_keep != nullptr) p.R_keep[slot * p.vecs + v] = r;
-                        if (p.Y_keep != nullptr) p.Y_keep[slot * p.vecs + v] = yq[u][j];
+                    for (int j = 0; j < kNV; ++j)
+                        if (in[j]) p.R[at[u] + j * threads] = r[j];
+                }
+                if (keep[u]) {
+#pragma unroll
+                    for (int j = 0; j < kNV; ++j) {
+                        if (!in[j]) continue;
+                        if (p.R_keep != nullptr) p.R_keep[slot[u] + j * threads] = r[j];
+                        if (p.Y_keep != nullptr) p.Y_keep[slot[u] + j * threads] = yq[u][j];
                     }
                 }
             }
             if (p.pre_w != nullptr) {
+                __syncwarp();
                 normalise(p.pre_w, p.pre_b);
 #pragma unroll
                 for (int u = 0; u < kU; ++u) {
-                    const int64_t row = row0 + u;
-                    const bool keep = row < hi && (kept >> (int)(row - lo) & 1u);
-                    const int64_t slot = place + __popc(kept & ((1u << (int)((row - lo) & 31)) - 1u));
+                    if (!live[u]) continue;
 #pragma unroll
                     for (int j = 0; j < kNV; ++j) {
-                        const int v = t + j * threads;
-                        if (v >= p.vecs || row >= hi) continue;
-                        const uint4 z = Vec<T>::pack(&x[u][j * VN]);
-                        if (p.Z != nullptr) p.Z[row * p.vecs + v] = z;
-                        if (keep && p.Z_keep != nullptr) p.Z_keep[slot * p.vecs + v] = z;
+                        if (!in[j]) continue;
+                        const uint4 z = Vec<T>::pack(&x[u][j * P]);
+                        if (p.Z != nullptr) p.Z[at[u] + j * threads] = z;
+                        if (keep[u] && p.Z_keep != nullptr) p.Z_keep[slot[u] + j * threads] = z;
                     }
                 }
             }
+            __syncwarp();
         }
     }
     // rows past M_keep of the caches are cleared
     if (p.caches) {
-        const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
         for (int64_t m = M_keep + worker; m < p.M_keep_cap; m += workers)
-            for (int v = t; v < p.vecs; v += threads) {
+            for (int v = kMulti ? (int)threadIdx.x : lane; v < p.vecs; v += kMulti ? (int)blockDim.x : 32) {
                 if (p.Y_keep != nullptr) p.Y_keep[m * p.vecs + v] = zero;
                 if (p.R_keep != nullptr) p.R_keep[m * p.vecs + v] = zero;
                 if (p.Z_keep != nullptr) p.Z_keep[m * p.vecs + v] = zero;
@@ -188,284 +215,322 @@ norm_forward_kernel(const NormFwdParams p) {
 }
 
 // ---- backward ----
+constexpr int kNormMaxC = 8192;
+constexpr int kNormSums = 5;                          // dpost_w, dpost_b, dpre_w, dpre_b, dgate
+constexpr int kNormMostWorkers = 15;                  // of a block, where each has a barrier of its own
 struct NormBwdParams {
     const uint4 *dR, *dZ, *R_keep, *Y_keep;
     const float *post_w, *post_b, *pre_w;
     const uint4* gate;
     uint4 *dH, *dY;
     const int32_t *keep_rows, *M_keep_dev, *status_word;
-    int64_t M, M_keep_cap, gate_group;
-    float* dgate;
-    float* sums;                                      // [kNormSums][workers][C]: dw_post, db_post, dw_pre, db_pre
+    int64_t M, M_keep_cap;
+    FastDiv gate_group;
+    float* dgate;                                     // (where it has more than one row: its sums leave a row at a time)
+    float* sums;                                      // [kNormSums][blocks][C]
     float* gate_sums;                                 // [workers][2][C]: first and last gate row of each worker
     int64_t workers;
-    int want;                                         // bits 0..3: those sums; 4: dgate
-    int vecs, warps, accumulate, copy_rest;
+    int want;                                         // bit k: sum k is wanted
+    int one_gate;                                     // the gate has one row: its gradient is a sum like the others
+    int vecs, warps, per_block, accumulate, copy_rest;               // warps of a worker (kLanes 0), workers of a block
     float scale, eps, inv_c;
 };
-constexpr int kNormSums = 4;
 
 __device__ __forceinline__ int64_t norm_chunk(int64_t M_keep, int64_t workers) { return (M_keep + workers - 1) / workers; }
 
-// A worker takes consecutive kept rows, kU at a time; a thread holds the same kNV vectors of every row, so that its share of
-// the weights' gradients stays in registers and leaves once, as a partial row that a second launch adds up.  The gate's
-// gradient is a sum over the rows of one gate row; the list is ascending, so a gate row's rows are consecutive: the sum is put
-// away when the gate row changes - straight into dgate where no other worker has rows of it (all but a worker's first and
-// last gate row).
-template <typename T, int kNV, int kU, bool kMulti, bool kLayer, bool kPost>
-__global__ void __launch_bounds__(kMulti ? 512 : 128, kMulti ? 1 : 4)
-norm_backward_kernel(const NormBwdParams p) {
-    constexpr int VN = Vec<T>::N;
-    constexpr int E = kNV * VN;
-    __shared__ float scratch[kMulti ? 2 * 32 * 3 * kU : 1];
+// Threads of a block, one block an SM: registers for rows of 8 numbers a thread, or of more.
+__host__ __device__ constexpr int norm_backward_threads(int numbers) { return numbers <= 8 ? 768 : 512; }
+
+// A worker - kLanes threads of a warp, or, kLanes 0, some warps - takes consecutive kept rows; a thread has the same kNV vectors of
+// each.  The weights' gradients are sums over rows: a worker's lie in shared memory, four numbers a thread and place, which only
+// that thread touches (five sums of 24 channels a thread do not fit in registers beside the row); at the end the block's workers are
+// added up and the block leaves one partial row for a second launch.  A warp has a whole row up to 1024 bf16 or 512 fp32 channels, so
+// that its sums need no barrier, and rows of few channels go several to a warp: what a row costs besides its numbers - three
+// rounds of sums over its threads, addresses, the gate row - was most of the instructions with one vector a thread.
+// The gate's gradient is a sum over the rows of one gate row; the list is ascending, so a gate row's rows are consecutive: the sum
+// is put away when the gate row changes - straight into dgate where no other worker has rows of it (all but a worker's first
+// and last gate row).
+template <typename T, int kNV, int kLanes, bool kFull, bool kLayer, bool kPost>
+__global__ void __launch_bounds__(norm_backward_threads(kNV * Vec<T>::N), 1) norm_backward_kernel(const NormBwdParams p) {
+    constexpr bool kMulti = kLanes == 0;
+    constexpr int VN = Vec<T>::N, P = VN / 2, E2 = kNV * P, kQ = VN / 4;      // kQ: float4 of a vector's sums
+    extern __shared__ float4 sums_s[];                // [worker of the block][wanted sum][vector of the thread][kQ][thread]
+    __shared__ float4 scratch[kMulti ? kNormMostWorkers * 32 : 1];
     pdl_launch_dependents();
     pdl_wait();
     if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
-    const int lane = threadIdx.x & 31;
-    const int64_t worker = kMulti ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
-    const int t = kMulti ? (int)threadIdx.x : lane, threads = kMulti ? (int)blockDim.x : 32;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int width = kMulti ? p.warps * 32 : kLanes, mine = threadIdx.x / width;          // threads of a worker; which one of the block
+    RowThreads<kLanes> row = {(int)threadIdx.x % width, width, p.warps, mine + 1, 0, scratch + mine * 32};
+    const int t = row.t, threads = row.threads();
+    const int64_t worker = (int64_t)blockIdx.x * p.per_block + mine;
     const int64_t M_keep = load_m_keep(p.M_keep_dev, p.M_keep_cap);
     const int64_t chunk = norm_chunk(M_keep, p.workers);
     const int64_t lo = worker * chunk < M_keep ? worker * chunk : M_keep, hi = lo + chunk < M_keep ? lo + chunk : M_keep;
-    int turn = 0;
-
-    if (worker < p.workers && lo < hi) {
-        float acc[kNormSums][E], gacc[E];
+    const int64_t C = (int64_t)p.vecs * VN;
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    const int per_sum = kNV * kQ * threads, wanted = __popc(p.want);
+    float4* own = sums_s + (int64_t)mine * wanted * per_sum + t;
+    float4* place[kNormSums];                         // of the wanted sums
 #pragma unroll
-        for (int e = 0; e < E; ++e) {
+    for (int k = 0; k < kNormSums; ++k) place[k] = own + __popc(p.want & ((1 << k) - 1)) * per_sum;
+    for (int i = 0; i < wanted * kNV * kQ; ++i) own[i * threads] = make_float4(0.f, 0.f, 0.f, 0.f);
+    bool in[kNV];
 #pragma unroll
-            for (int k = 0; k < kNormSums; ++k) acc[k][e] = 0.f;
-            gacc[e] = 0.f;
+    for (int j = 0; j < kNV; ++j) in[j] = kFull || t + j * threads < p.vecs;
+    auto accumulate = [&](float4* sum, int j, const f32x2* f) {
+#pragma unroll
+        for (int h = 0; h < kQ; ++h) {
+            float4* a = sum + (j * kQ + h) * threads;
+            const float4 old = *a;
+            const float2 u = both(add(pair(old.x, old.y), f[2 * h])), v = both(add(pair(old.z, old.w), f[2 * h + 1]));
+            *a = make_float4(u.x, u.y, v.x, v.y);
         }
-        const bool want_gate = p.want & 16;
-        int64_t first = 0, last = 0, cur = 0;
-        if (p.gate != nullptr) {
-            first = cur = mapped_row(p.keep_rows, lo) / p.gate_group;
-            last = mapped_row(p.keep_rows, hi - 1) / p.gate_group;
+    };
+    const bool gate_rows = (p.want & 16) && !p.one_gate;
+    uint32_t first = 0, last = 0, cur = 0;
+    if (p.gate != nullptr && lo < hi) {
+        first = cur = p.gate_group((uint32_t)mapped_row(p.keep_rows, lo) & 0x7fffffffu);
+        last = p.gate_group((uint32_t)mapped_row(p.keep_rows, hi - 1) & 0x7fffffffu);
+    }
+    auto put_gate = [&]() {                           // the gate row's sum, out of shared memory
+        const bool partial = cur == first || cur == last;
+        float* to = partial ? p.gate_sums + (worker * 2 + (cur == first ? 0 : 1)) * C : p.dgate + (int64_t)cur * C;
+#pragma unroll
+        for (int j = 0; j < kNV; ++j) {
+            if (!in[j]) continue;
+#pragma unroll
+            for (int h = 0; h < kQ; ++h) {
+                float4* a = place[4] + (j * kQ + h) * threads;
+                float4 s = *a;
+                *a = make_float4(0.f, 0.f, 0.f, 0.f);
+                float4* q = reinterpret_cast<float4*>(to + (int64_t)(t + j * threads) * VN) + h;
+                if (!partial && p.accumulate) {
+                    const float4 old = *q;
+                    s = make_float4(s.x + old.x, s.y + old.y, s.z + old.z, s.w + old.w);
+                }
+                *q = s;
+            }
         }
-        const int64_t C = (int64_t)p.vecs * VN;
-        auto put_gate = [&]() {
-            const bool partial = cur == first || cur == last;
-            float* to = partial ? p.gate_sums + (worker * 2 + (cur == first ? 0 : 1)) * C : p.dgate + cur * C;
-            const bool add = !partial && p.accumulate;
-#pragma unroll
-            for (int j = 0; j < kNV; ++j) {
-                const int v = t + j * threads;
-                if (v >= p.vecs) continue;
-#pragma unroll
-                for (int e = 0; e < VN; e += 4) {
-                    float4* q = reinterpret_cast<float4*>(to + (int64_t)v * VN + e);
-                    float4 s = make_float4(gacc[j * VN + e], gacc[j * VN + e + 1], gacc[j * VN + e + 2], gacc[j * VN + e + 3]);
-                    if (add) {
-                        const float4 old = *q;
-                        s.x += old.x;
-                        s.y += old.y;
-                        s.z += old.z;
-                        s.w += old.w;
-                    }
-                    *q = s;
-                }
-            }
-#pragma unroll
-            for (int e = 0; e < E; ++e) gacc[e] = 0.f;
-        };
-        for (int64_t m0 = lo; m0 < hi; m0 += kU) {
-            int64_t row[kU];
-            uint4 rq[kU][kNV], yq[kU][kNV], zq[kU][kNV], dq[kU][kNV];
-            const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                row[u] = m0 + u < hi ? (int64_t)mapped_row(p.keep_rows, m0 + u) : -1;
-                if (row[u] >= p.M) row[u] = -1;
-            }
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-#pragma unroll
-                for (int j = 0; j < kNV; ++j) {
-                    const int v = t + j * threads;
-                    const bool in = v < p.vecs && row[u] >= 0;
-                    rq[u][j] = in && p.dZ != nullptr ? ld_row(p.R_keep + (m0 + u) * p.vecs + v) : zero;
-                    zq[u][j] = in && p.dZ != nullptr ? ld_row(p.dZ + (m0 + u) * p.vecs + v) : zero;
-                    yq[u][j] = in && p.Y_keep != nullptr ? ld_row(p.Y_keep + (m0 + u) * p.vecs + v) : zero;
-                    dq[u][j] = in && p.dR != nullptr ? ld_row(p.dR + row[u] * p.vecs + v) : zero;
-                }
-            float x[kU][E], y[kU][E], g[kU][E];        // R, then what its norm makes of it; Y likewise; gradients
-            float wpre[E];
-#pragma unroll
-            for (int u = 0; u < kU; ++u)
-#pragma unroll
-                for (int j = 0; j < kNV; ++j) {
-                    Vec<T>::unpack(rq[u][j], &x[u][j * VN]);
-                    Vec<T>::unpack(yq[u][j], &y[u][j * VN]);
-                    Vec<T>::unpack(zq[u][j], &g[u][j * VN]);
-                }
-#pragma unroll
-            for (int j = 0; j < kNV; ++j) {
-                const int v = t + j * threads;
-#pragma unroll
-                for (int e = 0; e < VN; ++e) wpre[j * VN + e] = 0.f;
-                if (v < p.vecs && p.dZ != nullptr) load_f32<VN>(p.pre_w + v * VN, &wpre[j * VN]);
-            }
-            float s1[3 * kU], s2[3 * kU];
-            if constexpr (kLayer) {
-#pragma unroll
-                for (int u = 0; u < kU; ++u) {
-                    s1[3 * u] = s1[3 * u + 1] = s1[3 * u + 2] = 0.f;
-#pragma unroll
-                    for (int e = 0; e < E; ++e) {
-                        s1[3 * u] += x[u][e];
-                        if constexpr (kPost) s1[3 * u + 1] += y[u][e];
-                        s1[3 * u + 2] = fmaf(g[u][e], wpre[e], s1[3 * u + 2]);
-                    }
-                }
-                row_sums<3 * kU, kMulti>(s1, scratch, p.warps, turn);
-#pragma unroll
-                for (int u = 0; u < kU; ++u)
-#pragma unroll
-                    for (int j = 0; j < kNV; ++j) {
-                        const bool in = t + j * threads < p.vecs;            // threads past the row hold zeros, and keep them
-                        const float mx = in ? s1[3 * u] * p.inv_c : 0.f, my = in ? s1[3 * u + 1] * p.inv_c : 0.f;
-#pragma unroll
-                        for (int e = 0; e < VN; ++e) {
-                            x[u][j * VN + e] -= mx;
-                            if constexpr (kPost) y[u][j * VN + e] -= my;
-                        }
-                    }
-            }
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                s2[3 * u] = s2[3 * u + 1] = s2[3 * u + 2] = 0.f;
-#pragma unroll
-                for (int e = 0; e < E; ++e) {
-                    s2[3 * u] = fmaf(x[u][e], x[u][e], s2[3 * u]);
-                    if constexpr (kPost) s2[3 * u + 1] = fmaf(y[u][e], y[u][e], s2[3 * u + 1]);
-                    s2[3 * u + 2] = fmaf(g[u][e] * wpre[e], x[u][e], s2[3 * u + 2]);
-                }
-            }
-            row_sums<3 * kU, kMulti>(s2, scratch, p.warps, turn);
-            float s3[2 * kU], rstd_y[kU];
-#pragma unroll
-            for (int u = 0; u < kU; ++u) {
-                const float rstd = rsqrtf(fmaf(s2[3 * u], p.inv_c, p.eps));
-                rstd_y[u] = kPost ? rsqrtf(fmaf(s2[3 * u + 1], p.inv_c, p.eps)) : 1.f;
-                const float mg = kLayer ? s1[3 * u + 2] * p.inv_c : 0.f;
-                const float mgx = s2[3 * u + 2] * rstd * p.inv_c;             // mean of g n
-                s3[2 * u] = s3[2 * u + 1] = 0.f;
-                if (row[u] < 0) continue;
-                if (p.gate != nullptr && row[u] / p.gate_group != cur) {
-                    if (want_gate) put_gate();
-                    cur = row[u] / p.gate_group;
-                }
-#pragma unroll
-                for (int j = 0; j < kNV; ++j) {
-                    const int v = t + j * threads;
-                    if (v >= p.vecs) continue;
-                    float d[VN];
-                    Vec<T>::unpack(dq[u][j], d);
-#pragma unroll
-                    for (int e = 0; e < VN; ++e) {
-                        const int i = j * VN + e;
-                        const float n = x[u][i] * rstd, dz = g[u][i];
-                        acc[2][i] = fmaf(dz, n, acc[2][i]);
-                        acc[3][i] += dz;
-                        float q = dz * wpre[i];
-                        if (p.dZ != nullptr) d[e] = fmaf(rstd, q - mg - n * mgx, d[e]);
-                        g[u][i] = d[e];                                        // the whole gradient with respect to R
-                        d[e] *= p.scale;
-                    }
-                    if (p.dH != nullptr) p.dH[row[u] * p.vecs + v] = Vec<T>::pack(d);
-                    float wp[VN], bp[VN], gt[VN];
-                    if constexpr (kPost) {
-                        load_f32<VN>(p.post_w + v * VN, wp);
-                        if (p.post_b != nullptr) load_f32<VN>(p.post_b + v * VN, bp);
-                    }
-                    if (p.gate != nullptr) Vec<T>::unpack(__ldg(p.gate + cur * p.vecs + v), gt);
-#pragma unroll
-                    for (int e = 0; e < VN; ++e) {
-                        const int i = j * VN + e;
-                        const float n = y[u][i] * rstd_y[u];
-                        if (p.gate != nullptr) {
-                            float un = n;
-                            if constexpr (kPost) un = p.post_b != nullptr ? fmaf(n, wp[e], bp[e]) : n * wp[e];
-                            gacc[i] = fmaf(g[u][i], un, gacc[i]);
-                            g[u][i] *= gt[e];
-                        }
-                        if constexpr (kPost) {
-                            acc[0][i] = fmaf(g[u][i], n, acc[0][i]);
-                            acc[1][i] += g[u][i];
-                            y[u][i] = n;
-                            g[u][i] *= wp[e];
-                            s3[2 * u] += g[u][i];
-                            s3[2 * u + 1] = fmaf(g[u][i], n, s3[2 * u + 1]);
-                        }
-                    }
-                }
-            }
-            if constexpr (kPost) row_sums<2 * kU, kMulti>(s3, scratch, p.warps, turn);
+    };
+    auto total = [](f32x2 a) { return both(a).x + both(a).y; };
+    // (several rows a warp: every group of lanes goes round as often as the others, with nothing to do behind its last row)
+    constexpr bool kSplit = !kMulti && kLanes < 32;
+    const int rounds = kSplit ? (int)chunk : (int)(hi - lo);
+    int32_t next = lo < hi ? mapped_row(p.keep_rows, lo) : -1;
+    int64_t at = lo * p.vecs + t;
+    for (int i = 0; i < rounds; ++i, at += p.vecs) {
+        const bool have = !kSplit || lo + i < hi;
+        const int32_t k = next;
+        const bool live = have && k >= 0 && k < p.M;
+        next = lo + i + 1 < hi ? mapped_row(p.keep_rows, lo + i + 1) : -1;
+        if (!kSplit && !live) {                       // an entry outside the tensor is skipped
             if (p.dY != nullptr) {
 #pragma unroll
-                for (int u = 0; u < kU; ++u) {
-                    if (m0 + u >= hi) continue;
-                    const float mq = kLayer ? s3[2 * u] * p.inv_c : 0.f, mqn = s3[2 * u + 1] * p.inv_c;
+                for (int j = 0; j < kNV; ++j)
+                    if (in[j]) p.dY[at + j * threads] = zero;
+            }
+            continue;
+        }
+        const int64_t full = (int64_t)k * p.vecs + t;
+        f32x2 x[E2], y[E2], g[E2], q[E2];              // R, then what its norm makes of it; Y likewise; dZ; dZ pre_w
+        uint4 dq[kNV];
+        {
+            uint4 rq[kNV], yq[kNV], zq[kNV];
 #pragma unroll
-                    for (int j = 0; j < kNV; ++j) {
-                        const int v = t + j * threads;
-                        if (v >= p.vecs) continue;
-                        if constexpr (kPost) {
+            for (int j = 0; j < kNV; ++j) {
+                const bool ok = in[j] && live;
+                rq[j] = ok && p.dZ != nullptr ? __ldcg(p.R_keep + at + j * threads) : zero;
+                zq[j] = ok && p.dZ != nullptr ? __ldcg(p.dZ + at + j * threads) : zero;
+                yq[j] = ok && p.Y_keep != nullptr ? __ldcg(p.Y_keep + at + j * threads) : zero;
+                dq[j] = ok && p.dR != nullptr ? __ldcg(p.dR + full + j * threads) : zero;
+            }
 #pragma unroll
-                            for (int e = 0; e < VN; ++e) {
-                                const int i = j * VN + e;
-                                g[u][i] = rstd_y[u] * (g[u][i] - mq - y[u][i] * mqn);
-                            }
-                        }
-                        p.dY[(m0 + u) * p.vecs + v] = Vec<T>::pack(&g[u][j * VN]);
-                    }
+            for (int j = 0; j < kNV; ++j) {
+                f32x2 w[P];
+#pragma unroll
+                for (int e = 0; e < P; ++e) w[e] = pair(0.f, 0.f);
+                if (in[j] && p.dZ != nullptr) load_f32<VN>(p.pre_w + (t + j * threads) * VN, w);
+                Vec<T>::unpack(rq[j], &x[j * P]);
+                Vec<T>::unpack(yq[j], &y[j * P]);
+                Vec<T>::unpack(zq[j], &g[j * P]);
+#pragma unroll
+                for (int e = 0; e < P; ++e) q[j * P + e] = mul(g[j * P + e], w[e]);
+            }
+        }
+        float s1[3] = {0.f, 0.f, 0.f}, s2[3];
+        if constexpr (kLayer) {
+            f32x2 sx = x[0], sy = y[0], sq = q[0];
+#pragma unroll
+            for (int e = 1; e < E2; ++e) {
+                sx = add(sx, x[e]);
+                if constexpr (kPost) sy = add(sy, y[e]);
+                sq = add(sq, q[e]);
+            }
+            s1[0] = total(sx);
+            s1[1] = kPost ? total(sy) : 0.f;
+            s1[2] = total(sq);
+            row.sums(s1);
+#pragma unroll
+            for (int j = 0; j < kNV; ++j) {
+                const float mx = in[j] ? -s1[0] * p.inv_c : 0.f, my = in[j] ? -s1[1] * p.inv_c : 0.f;       // threads past the row keep zeros
+#pragma unroll
+                for (int e = j * P; e < (j + 1) * P; ++e) {
+                    x[e] = add(x[e], pair(mx, mx));
+                    if constexpr (kPost) y[e] = add(y[e], pair(my, my));
                 }
             }
         }
-        if (want_gate) put_gate();
+        {
+            f32x2 sx = mul(x[0], x[0]), sy = mul(y[0], y[0]), sq = mul(q[0], x[0]);
 #pragma unroll
-        for (int k = 0; k < kNormSums; ++k) {
-            if (!(p.want >> k & 1)) continue;
-            float* to = p.sums + ((int64_t)k * p.workers + worker) * C;
-#pragma unroll
-            for (int j = 0; j < kNV; ++j) {
-                const int v = t + j * threads;
-                if (v >= p.vecs) continue;
-#pragma unroll
-                for (int e = 0; e < VN; e += 4)
-                    *reinterpret_cast<float4*>(to + (int64_t)v * VN + e) =
-                        make_float4(acc[k][j * VN + e], acc[k][j * VN + e + 1], acc[k][j * VN + e + 2], acc[k][j * VN + e + 3]);
+            for (int e = 1; e < E2; ++e) {
+                sx = fma(x[e], x[e], sx);
+                if constexpr (kPost) sy = fma(y[e], y[e], sy);
+                sq = fma(q[e], x[e], sq);
+            }
+            s2[0] = total(sx);
+            s2[1] = kPost ? total(sy) : 0.f;
+            s2[2] = total(sq);
+            row.sums(s2);
+        }
+        const float rstd = rsqrtf(fmaf(s2[0], p.inv_c, p.eps)), rstd_y = kPost ? rsqrtf(fmaf(s2[1], p.inv_c, p.eps)) : 1.f;
+        // d + rstd (q - mean(q) - n mean(q n)), n = rstd x
+        const float k0 = kLayer ? -s1[2] * p.inv_c * rstd : 0.f, k1 = -(s2[2] * p.inv_c * rstd) * rstd;
+        if (live && p.gate != nullptr) {
+            const uint32_t group = p.gate_group((uint32_t)k);
+            if (group != cur) {
+                if (gate_rows) put_gate();
+                cur = group;
             }
         }
+        f32x2 sq = pair(0.f, 0.f), sqn = pair(0.f, 0.f);
+        if (live) {
+            const f32x2 rr = pair(rstd, rstd);
+#pragma unroll
+            for (int j = 0; j < kNV; ++j) {
+                if (!in[j]) continue;
+                f32x2 out[P], d[P], w[P], b[P];
+                Vec<T>::unpack(dq[j], d);
+                if (p.dZ != nullptr) {
+#pragma unroll
+                    for (int e = 0; e < P; ++e) {
+                        const f32x2 n = mul(x[j * P + e], rr);
+                        d[e] = add(d[e], fma(q[j * P + e], rr, fma(n, pair(k1, k1), pair(k0, k0))));        // the whole gradient of R
+                        out[e] = mul(g[j * P + e], n);
+                    }
+                    if (p.want & 4) accumulate(place[2], j, out);
+                    if (p.want & 8) accumulate(place[3], j, &g[j * P]);
+                }
+                if (p.dH != nullptr) {
+#pragma unroll
+                    for (int e = 0; e < P; ++e) out[e] = mul(d[e], pair(p.scale, p.scale));
+                    p.dH[full + j * threads] = Vec<T>::pack(out);
+                }
+                if constexpr (kPost) {
+                    load_f32<VN>(p.post_w + (t + j * threads) * VN, w);
+#pragma unroll
+                    for (int e = 0; e < P; ++e) y[j * P + e] = mul(y[j * P + e], pair(rstd_y, rstd_y));
+                }
+                if (p.gate != nullptr) {
+                    if (p.want & 16) {
+                        if constexpr (kPost)
+                            if (p.post_b != nullptr) load_f32<VN>(p.post_b + (t + j * threads) * VN, b);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) {
+                            f32x2 u = y[j * P + e];
+                            if constexpr (kPost) u = p.post_b != nullptr ? fma(u, w[e], b[e]) : mul(u, w[e]);
+                            out[e] = mul(d[e], u);
+                        }
+                        accumulate(place[4], j, out);
+                    }
+                    Vec<T>::unpack(__ldg(p.gate + (int64_t)cur * p.vecs + t + j * threads), b);
+#pragma unroll
+                    for (int e = 0; e < P; ++e) d[e] = mul(d[e], b[e]);
+                }
+                if constexpr (kPost) {
+                    if (p.want & 1) {
+#pragma unroll
+                        for (int e = 0; e < P; ++e) out[e] = mul(d[e], y[j * P + e]);
+                        accumulate(place[0], j, out);
+                    }
+                    if (p.want & 2) accumulate(place[1], j, d);
+#pragma unroll
+                    for (int e = 0; e < P; ++e) {
+                        d[e] = mul(d[e], w[e]);
+                        sq = add(sq, d[e]);
+                        sqn = fma(d[e], y[j * P + e], sqn);
+                    }
+                }
+#pragma unroll
+                for (int e = 0; e < P; ++e) g[j * P + e] = d[e];
+            }
+        }
+        if constexpr (kSplit) __syncwarp();
+        float s3[2] = {total(sq), total(sqn)};
+        if constexpr (kPost) row.sums(s3);
+        if (p.dY != nullptr && have) {
+            const float c0 = kLayer ? -s3[0] * p.inv_c * rstd_y : 0.f, c1 = -s3[1] * p.inv_c * rstd_y;
+#pragma unroll
+            for (int j = 0; j < kNV; ++j) {
+                if (!in[j]) continue;
+                if constexpr (kPost) {
+#pragma unroll
+                    for (int e = j * P; e < (j + 1) * P; ++e) g[e] = fma(g[e], pair(rstd_y, rstd_y), fma(y[e], pair(c1, c1), pair(c0, c0)));
+                }
+                p.dY[at + j * threads] = live ? Vec<T>::pack(&g[j * P]) : zero;
+            }
+        }
+        if constexpr (kSplit) __syncwarp();
     }
-    if (worker >= p.workers) return;
+    if (gate_rows && lo < hi) put_gate();
+    // the block's workers together, in their order
+    __syncthreads();
+    for (int i = threadIdx.x; i < wanted * per_sum; i += blockDim.x) {
+        const int which = i / per_sum, rest = i - which * per_sum;   // (sum, (vector, quarter), thread)
+        int k = p.want;                                              // the which-th bit that is set
+        for (int b = 0; b < which; ++b) k &= k - 1;
+        k = __ffs(k) - 1;
+        if (k == 4 && !p.one_gate) continue;
+        const int jh = rest / threads, v = rest % threads + jh / kQ * threads;
+        if (v >= p.vecs) continue;
+        float4 s = sums_s[i];
+        for (int w = 1; w < p.per_block; ++w) {
+            const float4 q = sums_s[(int64_t)w * wanted * per_sum + i];
+            s = make_float4(s.x + q.x, s.y + q.y, s.z + q.z, s.w + q.w);
+        }
+        reinterpret_cast<float4*>(p.sums + ((int64_t)k * gridDim.x + blockIdx.x) * C + (int64_t)v * VN)[jh % kQ] = s;
+    }
+    const int64_t warps = (int64_t)gridDim.x * (blockDim.x >> 5), me = (int64_t)blockIdx.x * (blockDim.x >> 5) + warp;
     if (p.dY != nullptr) {                            // rows past M_keep are cleared
-        for (int64_t m = M_keep + worker; m < p.M_keep_cap; m += p.workers)
-            for (int v = t; v < p.vecs; v += threads) p.dY[m * p.vecs + v] = make_uint4(0u, 0u, 0u, 0u);
+        for (int64_t m = M_keep + me; m < p.M_keep_cap; m += warps)
+            for (int v = lane; v < p.vecs; v += 32) p.dY[m * p.vecs + v] = zero;
     }
     // the rows outside the list take the residual's gradient alone; every warp has its share of all rows
     if (p.copy_rest) {
-        const int64_t warps = p.workers * p.warps, warp = kMulti ? worker * p.warps + (threadIdx.x >> 5) : worker;
-        const int64_t from = p.M * warp / warps, to = p.M * (warp + 1) / warps;
+        const int64_t from = p.M * me / warps, to = p.M * (me + 1) / warps;
         warp_visit_dropped_rows(p.keep_rows, M_keep, from, to, lane, [&](int64_t base, uint32_t todo) {
+            // four rows at a time, 32 vectors of each: their loads before their stores
+            constexpr int kB = 4;
             while (todo) {
-                const int64_t r = base + __ffs(todo) - 1;
-                todo &= todo - 1;
-                constexpr int kB = 4;
-                for (int v0 = lane; v0 < p.vecs; v0 += 32 * kB) {
-                    uint4 q[kB];
+                int64_t at[kB];
 #pragma unroll
-                    for (int b = 0; b < kB; ++b)
-                        q[b] = v0 + 32 * b < p.vecs && p.dR != nullptr ? ld_row(p.dR + r * p.vecs + v0 + 32 * b) : make_uint4(0u, 0u, 0u, 0u);
+                for (int b = 0; b < kB; ++b) {
+                    at[b] = todo ? (base + __ffs(todo) - 1) * p.vecs : -1;
+                    todo &= todo - 1;
+                }
+                for (int v0 = lane; v0 < p.vecs; v0 += 32) {
+                    uint4 v[kB];
+#pragma unroll
+                    for (int b = 0; b < kB; ++b) v[b] = at[b] >= 0 && p.dR != nullptr ? __ldcg(p.dR + at[b] + v0) : zero;
 #pragma unroll
                     for (int b = 0; b < kB; ++b) {
-                        if (v0 + 32 * b >= p.vecs) continue;
-                        float f[VN];
-                        Vec<T>::unpack(q[b], f);
+                        if (at[b] < 0) continue;
+                        f32x2 f[P];
+                        Vec<T>::unpack(v[b], f);
 #pragma unroll
-                        for (int e = 0; e < VN; ++e) f[e] *= p.scale;
-                        p.dH[r * p.vecs + v0 + 32 * b] = Vec<T>::pack(f);
+                        for (int e = 0; e < P; ++e) f[e] = mul(f[e], pair(p.scale, p.scale));
+                        p.dH[at[b] + v0] = Vec<T>::pack(f);
                     }
                 }
             }
@@ -473,131 +538,176 @@ norm_backward_kernel(const NormBwdParams p) {
     }
 }
 
-// Adds the workers' partial rows in a fixed order.  A block makes 256 / slices columns of one output: slice i takes partial rows
-// i, i + slices, ..., and the slices are added as a tree.
+// Adds the blocks' partial rows in a fixed order - 32 columns a block, slice i of 32 takes rows i, i + 32, ..., and the slices are added
+// as a tree - and, for a gate of several rows, the workers' partial rows of each: the same, or, where a gate row has few workers,
+// 256 columns of four gate rows a block.
+constexpr int kReduceThreads = 1024, kReduceSlices = 32;
 struct NormReduceParams {
     const float *sums, *gate_sums;
     float* out[kNormSums];
-    float* dgate;
+    float* dgate;                                     // of several rows, else nullptr
     const int32_t *keep_rows, *M_keep_dev, *status_word;
-    int64_t M_keep_cap, workers, groups, gate_group;
-    int C, accumulate, slices, gate_slices, sum_tiles, gate_tiles;       // column tiles of a sum / of a gate row
+    int64_t M_keep_cap, workers, gate_group, gate_rows;
+    int C, accumulate, blocks, few_workers, tiles, gate_tiles;       // column tiles of a sum / of a gate row
+    int outputs, output[kNormSums];                                  // which of the sums are wanted
 };
-__global__ void __launch_bounds__(256) norm_reduce_kernel(const NormReduceParams p) {
-    __shared__ float part[256];
+__device__ __forceinline__ float add_rows(const float* from, int64_t stride, int64_t n) {
+    float s = 0.f;
+    int64_t i = 0;
+    for (; i + 8 <= n; i += 8) {
+        float f[8];
+#pragma unroll
+        for (int u = 0; u < 8; ++u) f[u] = __ldg(from + (i + u) * stride);
+#pragma unroll
+        for (int u = 0; u < 8; ++u) s += f[u];
+    }
+    for (; i < n; ++i) s += __ldg(from + i * stride);
+    return s;
+}
+__global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormReduceParams p) {
+    __shared__ float part[kReduceThreads];
     pdl_launch_dependents();
     pdl_wait();
     if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
-    const int64_t M_keep = load_m_keep(p.M_keep_dev, p.M_keep_cap);
-    const int64_t chunk = norm_chunk(M_keep, p.workers);
-    const int64_t used = chunk > 0 ? (M_keep + chunk - 1) / chunk : 0;
-    const bool is_sum = blockIdx.x < (unsigned)(kNormSums * p.sum_tiles);
-    const int slices = is_sum ? p.slices : p.gate_slices;
-    const int cols = 256 / slices, col = threadIdx.x % cols, slice = threadIdx.x / cols;
-    float* out;
-    int64_t w0, w1, a = 0, c0;
-    int64_t group = -1;
-    if (is_sum) {
-        const int k = blockIdx.x / p.sum_tiles;
+    const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
+    float *out = nullptr, s = 0.f;
+    int64_t c;
+    bool tree = true;
+    if (blockIdx.x < (unsigned)(p.outputs * p.tiles)) {
+        const int k = p.output[blockIdx.x / p.tiles];
         out = p.out[k];
-        if (out == nullptr) return;
-        c0 = (int64_t)(blockIdx.x % p.sum_tiles) * cols;
-        w0 = 0;
-        w1 = used;
-        a = k;
+        c = (int64_t)(blockIdx.x % p.tiles) * 32 + lane;
+        if (c < p.C && slice < p.blocks)
+            s = add_rows(p.sums + ((int64_t)k * p.blocks + slice) * p.C + c, (int64_t)kReduceSlices * p.C, (p.blocks - slice + kReduceSlices - 1) / kReduceSlices);
     } else {
-        const int64_t id = (int64_t)blockIdx.x - kNormSums * p.sum_tiles;
-        group = id / p.gate_tiles;
-        c0 = id % p.gate_tiles * cols;
-        out = p.dgate + group * p.C;
-        // the kept rows [a, b) of this gate row, and the workers that had them
-        const int64_t r0 = group * p.gate_group, r1 = r0 + p.gate_group;
-        int64_t b;
-        if (p.keep_rows == nullptr) {
-            a = r0 < M_keep ? r0 : M_keep;
-            b = r1 < M_keep ? r1 : M_keep;
-        } else {
-            a = warp_lower_bound(p.keep_rows, M_keep, r0, threadIdx.x & 31);
-            b = warp_lower_bound(p.keep_rows, M_keep, r1, threadIdx.x & 31);
+        const int64_t M_keep = load_m_keep(p.M_keep_dev, p.M_keep_cap), chunk = norm_chunk(M_keep, p.workers);
+        const int64_t id = (int64_t)blockIdx.x - p.outputs * p.tiles;
+        int64_t group = id / p.gate_tiles, step = kReduceSlices, start = slice;
+        c = id % p.gate_tiles * 32 + lane;
+        if (p.few_workers) {
+            tree = false;
+            group = group * 4 + (threadIdx.x >> 8);
+            c = id % p.gate_tiles * 256 + (threadIdx.x & 255);
+            step = 1;
+            start = 0;
         }
-        w0 = a < b ? a / chunk : 0;
-        w1 = a < b ? (b - 1) / chunk + 1 : 0;
-        if (w1 - w0 == 1 && a > w0 * chunk && b < (w0 + 1) * chunk && b < M_keep) return;       // inside one worker's rows: already written
-    }
-    const int64_t c = c0 + col;
-    float s = 0.f;
-    if (c < p.C) {
-#pragma unroll 8
-        for (int64_t w = w0 + slice; w < w1; w += slices) {
-            // a worker that begins before this gate row has it as its last one
-            const float* from = is_sum ? p.sums + (a * p.workers + w) * p.C : p.gate_sums + (w * 2 + (w * chunk < a ? 1 : 0)) * p.C;
-            s += __ldg(from + c);
+        if (group < p.gate_rows) {
+            // the kept rows [a, b) of this gate row, and the workers that had them
+            const int64_t r0 = group * p.gate_group, r1 = r0 + p.gate_group;
+            int64_t a, b;
+            if (p.keep_rows == nullptr) {
+                a = r0 < M_keep ? r0 : M_keep;
+                b = r1 < M_keep ? r1 : M_keep;
+            } else {
+                a = warp_lower_bound(p.keep_rows, M_keep, r0, lane);
+                b = warp_lower_bound(p.keep_rows, M_keep, r1, lane);
+            }
+            const int64_t w0 = a < b ? a / chunk : 0, w1 = a < b ? (b - 1) / chunk + 1 : 0;
+            // inside one worker's rows it is already written
+            if (!(w1 - w0 == 1 && a > w0 * chunk && b < (w0 + 1) * chunk && b < M_keep)) out = p.dgate + group * p.C;
+            // a worker that begins before this gate row has it as its last one, the others as their first
+            const float* from = p.gate_sums + c;
+            const int64_t inner = w0 + (a < b && w0 * chunk < a ? 1 : 0);
+            if (out != nullptr && c < p.C) {
+                if (inner > w0 && start == 0) s = __ldg(from + (w0 * 2 + 1) * p.C);
+                if (inner + start < w1) s += add_rows(from + (inner + start) * 2 * p.C, step * 2 * p.C, (w1 - inner - start + step - 1) / step);
+            }
         }
     }
-    part[threadIdx.x] = s;
-    for (int h = slices / 2; h > 0; h /= 2) {
-        __syncthreads();
-        if (slice < h) part[threadIdx.x] += part[threadIdx.x + h * cols];
+    if (tree) {
+        part[threadIdx.x] = s;
+        for (int h = kReduceSlices / 2; h > 0; h /= 2) {
+            __syncthreads();
+            if (slice < h) part[threadIdx.x] += part[threadIdx.x + h * 32];
+        }
+        if (slice != 0) return;
+        s = part[threadIdx.x];
     }
-    if (slice == 0 && c < p.C) out[c] = part[threadIdx.x] + (p.accumulate ? out[c] : 0.f);
+    if (out != nullptr && c < p.C) out[c] = s + (p.accumulate ? out[c] : 0.f);
 }
 
 // ---- host ----
-constexpr int kNormMaxC = 8192;
+// (a gate row of M rows or more is the only one)
+inline FastDiv group_div(const void* gate, int64_t gate_group, int64_t M) { return FastDiv(gate == nullptr ? 1u : (uint32_t)(gate_group < M ? gate_group : M)); }
 
 struct NormShape {
-    int vecs, nv, warps;                              // vectors of a row, vectors a thread holds, warps a row
+    int vecs, nv, lanes, warps, per;                  // vectors of a row, of a thread; lanes of a row (0: warps of it); numbers of a vector
 };
-// most vectors a thread holds: forward 32 bf16 or 16 fp32 numbers (a warp a row up to 1024 bf16 or 512 fp32 channels), backward
-// 8 numbers, which leave room for the five sums, and 16 only where a row would need more than sixteen warps
+// Eight numbers a thread up to 1024 channels: several rows a warp up to 128 channels, several warps a row from 256 on.  (Rows of up to
+// 1024 channels in one warp, up to 32 numbers a thread, take fewer instructions but leave registers for 14 warps an SM, which
+// spend ten cycles an instruction: 25088 x 768 forward 52 us.)  Beyond, 16 or 32 numbers.
 inline NormShape norm_shape(sbp_dtype dt, int64_t C, bool backward) {
     NormShape s;
-    const int per = dt == SBP_BF16 ? 8 : 4;
-    s.vecs = (int)(C / per);
-    if (!backward) {
-        s.nv = 4;
-        s.warps = s.vecs <= 128 ? 1 : (s.vecs + 127) / 128;
-        if (s.warps == 1) s.nv = (s.vecs + 31) / 32;
-    } else {
-        s.nv = dt == SBP_BF16 ? 1 : 2;
-        if (s.vecs <= 32) s.nv = 1;
-        if ((s.vecs + 32 * s.nv - 1) / (32 * s.nv) > 16) s.nv *= 2;
-        s.warps = (s.vecs + 32 * s.nv - 1) / (32 * s.nv);
-    }
+    s.per = dt == SBP_BF16 ? 8 : 4;
+    s.vecs = (int)(C / s.per);
+    s.lanes = C <= 64 ? 8 : C <= 128 ? 16 : C <= 256 ? 32 : 0;
+    s.nv = C <= 1024 ? 8 / s.per : backward && dt == SBP_BF16 ? 2 : 4;
+    s.warps = s.lanes > 0 ? 1 : (s.vecs + 32 * s.nv - 1) / (32 * s.nv);
     return s;
 }
-inline int64_t norm_backward_workers(const NormShape& s, int64_t M_keep_cap) {
-    const int64_t most = (int64_t)kNumSMs * (s.warps == 1 ? 16 : s.warps < 16 ? 16 / s.warps : 1);
-    const int64_t want = (M_keep_cap + 1) / 2;
-    return want < 1 ? 1 : want < most ? want : most;
+// Backward blocks: as many workers as the sums of one leave room for in shared memory, up to 16 warps
+constexpr size_t kNormSmem = 200 * 1024;
+static_assert(kNormSmem >= (size_t)kNormSums * kNormMaxC * 4, "the sums of one worker");
+inline int norm_per_block(const NormShape& s, int sums) {
+    const int threads = s.lanes > 0 ? s.lanes : 32 * s.warps;
+    const size_t bytes = (size_t)(sums > 0 ? sums : 1) * threads * s.nv * s.per * 4;
+    int64_t n = (int64_t)(kNormSmem / bytes);
+    const int most = norm_backward_threads(s.nv * s.per) / threads;
+    if (n > most) n = most;
+    if (s.lanes > 0) n = n / (32 / s.lanes) * (32 / s.lanes);        // whole warps
+    else if (n > kNormMostWorkers) n = kNormMostWorkers;
+    return n < 1 ? 1 : (int)n;
 }
 
-template <typename T, int kNV, int kU, bool kMulti>
-cudaError_t launch_norm_forward(const NormFwdParams& p, bool layer, bool post, dim3 grid, dim3 block, cudaStream_t stream) {
-    if (layer)
-        return post ? launch_pdl(norm_forward_kernel<T, kNV, kU, kMulti, true, true>, grid, block, 0, stream, p)
-                    : launch_pdl(norm_forward_kernel<T, kNV, kU, kMulti, true, false>, grid, block, 0, stream, p);
-    return post ? launch_pdl(norm_forward_kernel<T, kNV, kU, kMulti, false, true>, grid, block, 0, stream, p)
-                : launch_pdl(norm_forward_kernel<T, kNV, kU, kMulti, false, false>, grid, block, 0, stream, p);
+struct NormGrid {
+    int blocks, per_block;
+    int64_t workers;
+};
+// a block an SM; few rows: as many workers as rows (or as a quarter of the rows outside the list), over the blocks evenly
+inline NormGrid norm_grid(const NormShape& s, int sums, int64_t M, int64_t M_keep_cap) {
+    NormGrid g;
+    if ((M - M_keep_cap + 3) / 4 > M_keep_cap) M_keep_cap = (M - M_keep_cap + 3) / 4;
+    g.per_block = norm_per_block(s, sums);
+    const int64_t step = s.lanes > 0 ? 32 / s.lanes : 1;             // workers of a warp
+    const int64_t each = (M_keep_cap + kNumSMs - 1) / kNumSMs, even = (each + step - 1) / step * step;
+    if (even < g.per_block) g.per_block = even < step ? (int)step : (int)even;
+    const int64_t blocks = (M_keep_cap + g.per_block - 1) / g.per_block;
+    g.blocks = (int)(blocks < 1 ? 1 : blocks < kNumSMs ? blocks : kNumSMs);
+    g.workers = (int64_t)g.blocks * g.per_block;
+    return g;
 }
-template <typename T>
-cudaError_t pick_norm_forward(const NormShape& s, const NormFwdParams& p, bool layer, bool post, dim3 grid, dim3 block, cudaStream_t stream) {
-    if (s.warps > 1) return launch_norm_forward<T, 4, 1, true>(p, layer, post, grid, block, stream);
-    switch (s.nv) {
-        case 1: return launch_norm_forward<T, 1, 4, false>(p, layer, post, grid, block, stream);
-        case 2: return launch_norm_forward<T, 2, 2, false>(p, layer, post, grid, block, stream);
-        case 3: return launch_norm_forward<T, 3, 1, false>(p, layer, post, grid, block, stream);
-        default: return launch_norm_forward<T, 4, 1, false>(p, layer, post, grid, block, stream);
-    }
+
+template <typename T, int kNV, int kLanes, bool kFull, typename Params>
+cudaError_t launch_norm(const Params& p, bool layer, bool post, dim3 grid, dim3 block, size_t smem, cudaStream_t stream) {
+    auto with = [&](auto layer_c, auto post_c) {
+        if constexpr (std::is_same_v<Params, NormFwdParams>) {
+            return launch_pdl(norm_forward_kernel<T, kNV, kLanes, kFull, decltype(layer_c)::value, decltype(post_c)::value>, grid, block, smem, stream, p);
+        } else {
+            constexpr auto kernel = norm_backward_kernel<T, kNV, kLanes, kFull, decltype(layer_c)::value, decltype(post_c)::value>;
+            const cudaError_t e = opt_in_dynamic_smem<kernel>((int)kNormSmem);
+            return e == cudaSuccess ? launch_pdl(kernel, grid, block, smem, stream, p) : e;
+        }
+    };
+    if (layer) return post ? with(std::true_type(), std::true_type()) : with(std::true_type(), std::false_type());
+    return post ? with(std::false_type(), std::true_type()) : with(std::false_type(), std::false_type());
 }
-template <typename T, int kNV, bool kMulti>
-cudaError_t launch_norm_backward_kernel(const NormBwdParams& p, bool layer, bool post, dim3 grid, dim3 block, cudaStream_t stream) {
-    constexpr int kU = kNV * Vec<T>::N <= 4 ? 2 : 1;
-    if (layer)
-        return post ? launch_pdl(norm_backward_kernel<T, kNV, kU, kMulti, true, true>, grid, block, 0, stream, p)
-                    : launch_pdl(norm_backward_kernel<T, kNV, kU, kMulti, true, false>, grid, block, 0, stream, p);
-    return post ? launch_pdl(norm_backward_kernel<T, kNV, kU, kMulti, false, true>, grid, block, 0, stream, p)
-                : launch_pdl(norm_backward_kernel<T, kNV, kU, kMulti, false, false>, grid, block, 0, stream, p);
+// the shapes that norm_shape makes
+template <typename T, typename Params>
+cudaError_t pick_norm(const NormShape& s, const Params& p, bool layer, bool post, dim3 grid, dim3 block, size_t smem, cudaStream_t stream) {
+    constexpr bool kBackward = std::is_same_v<Params, NormBwdParams>, kWide = std::is_same_v<T, float>;
+    const bool full = s.vecs == s.nv * (s.lanes > 0 ? s.lanes : 32 * s.warps);
+    auto with = [&](auto nv, auto lanes) {
+        return full ? launch_norm<T, decltype(nv)::value, decltype(lanes)::value, true>(p, layer, post, grid, block, smem, stream)
+                    : launch_norm<T, decltype(nv)::value, decltype(lanes)::value, false>(p, layer, post, grid, block, smem, stream);
+    };
+    constexpr std::integral_constant<int, kWide ? 2 : 1> eight;      // vectors of eight numbers
+    if (s.lanes == 8) return with(eight, std::integral_constant<int, 8>());
+    if (s.lanes == 16) return with(eight, std::integral_constant<int, 16>());
+    if (s.lanes == 32) return with(eight, std::integral_constant<int, 32>());
+    const std::integral_constant<int, 0> warps;
+    if (s.nv == eight) return with(eight, warps);
+    if constexpr (kBackward && !kWide) return with(std::integral_constant<int, 2>(), warps);
+    else return with(std::integral_constant<int, 4>(), warps);
 }
 
 }  // namespace
@@ -618,7 +728,7 @@ cudaError_t launch_block_norm_forward(sbp_dtype dt, bool layer, const void* H, c
     p.pre_w = pre_w;
     p.pre_b = pre_b;
     p.gate = (const uint4*)gate;
-    p.gate_group = gate_group;
+    p.gate_group = group_div(gate, gate_group, M);
     p.R = (uint4*)R;
     p.Z = (uint4*)Z;
     p.Y_keep = (uint4*)Y_keep;
@@ -631,22 +741,30 @@ cudaError_t launch_block_norm_forward(sbp_dtype dt, bool layer, const void* H, c
     p.status_word = status_word;
     p.M = M;
     p.vecs = s.vecs;
-    p.warps = s.warps;
     p.scale = scale;
     p.eps = eps;
     p.inv_c = 1.f / (float)C;
-    const int per_block = s.warps > 1 ? 1 : 8;
-    // rows a worker: enough workers for several waves, and never more rows than the mask of kept rows has bits
-    const int64_t chunk = s.warps > 1 ? 1 : M >= 4 * 148 * 24 ? 4 : M >= 2 * 148 * 24 ? 2 : 1;
+    // rows a warp (a block, for long rows): enough of them for several waves, and never more rows than the mask of kept rows has bits
+    const bool multi = s.lanes == 0;
+    const int64_t groups = multi ? 1 : 32 / s.lanes, waves = M / (groups * kNumSMs * (multi ? 4 : 48));
+    const int64_t chunk = groups * (waves >= 4 ? 4 : waves >= 2 ? 2 : 1), workers = (M + chunk - 1) / chunk;
     p.chunk = (int)chunk;
-    const int64_t workers = (M + chunk - 1) / chunk;
-    const dim3 grid((unsigned)((workers + per_block - 1) / per_block)), block(32 * (s.warps > 1 ? s.warps : per_block));
-    return dt == SBP_BF16 ? pick_norm_forward<__nv_bfloat16>(s, p, layer, post_w != nullptr, grid, block, stream)
-                          : pick_norm_forward<float>(s, p, layer, post_w != nullptr, grid, block, stream);
+    const int per_block = multi ? 1 : 8;
+    const dim3 grid((unsigned)((workers + per_block - 1) / per_block)), block(32 * (multi ? s.warps : per_block));
+    return dt == SBP_BF16 ? pick_norm<__nv_bfloat16>(s, p, layer, post_w != nullptr, grid, block, 0, stream)
+                          : pick_norm<float>(s, p, layer, post_w != nullptr, grid, block, 0, stream);
 }
 
-size_t block_norm_backward_workspace_bytes(sbp_dtype dt, int64_t M_keep_cap, int64_t C) {
-    return (size_t)norm_backward_workers(norm_shape(dt, C, true), M_keep_cap) * (kNormSums + 2) * (size_t)C * sizeof(float);
+size_t block_norm_backward_workspace_bytes(sbp_dtype dt, int64_t M, int64_t M_keep_cap, int64_t C) {
+    // (fewer sums leave room for more workers a block)
+    const NormShape s = norm_shape(dt, C, true);
+    size_t most = 0;
+    for (int sums = 1; sums <= kNormSums; ++sums) {
+        const NormGrid g = norm_grid(s, sums, M, M_keep_cap);
+        const size_t rows = (size_t)kNormSums * g.blocks + 2 * (size_t)g.workers;
+        most = rows > most ? rows : most;
+    }
+    return most * (size_t)C * sizeof(float);
 }
 
 cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR, const void* dZ, const void* R_keep, const void* Y_keep,
@@ -665,7 +783,7 @@ cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR,
     p.post_b = post_b;
     p.pre_w = pre_w;
     p.gate = (const uint4*)gate;
-    p.gate_group = gate_group;
+    p.gate_group = group_div(gate, gate_group, M);
     p.dH = (uint4*)dH;
     p.dY = (uint4*)dY;
     p.keep_rows = keep_rows;
@@ -674,10 +792,16 @@ cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR,
     p.M = M;
     p.M_keep_cap = M_keep_cap;
     p.dgate = dgate;
-    p.workers = norm_backward_workers(s, M_keep_cap);
-    p.sums = workspace;
-    p.gate_sums = workspace + (size_t)kNormSums * p.workers * C;
     p.want = (dpost_w ? 1 : 0) | (dpost_b ? 2 : 0) | (dpre_w ? 4 : 0) | (dpre_b ? 8 : 0) | (dgate ? 16 : 0);
+    const int64_t gate_rows = dgate != nullptr ? (M + gate_group - 1) / gate_group : 0;
+    p.one_gate = gate_rows == 1;
+    int sums = 0;
+    for (int k = 0; k < kNormSums; ++k) sums += p.want >> k & 1;
+    const NormGrid g = norm_grid(s, sums, M, M_keep_cap);
+    p.per_block = g.per_block;
+    p.workers = g.workers;
+    p.sums = workspace;
+    p.gate_sums = workspace + (size_t)kNormSums * g.blocks * C;
     p.vecs = s.vecs;
     p.warps = s.warps;
     p.accumulate = accumulate;
@@ -685,20 +809,12 @@ cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR,
     p.scale = scale;
     p.eps = eps;
     p.inv_c = 1.f / (float)C;
-    const int per_block = s.warps > 1 ? 1 : 4;
-    const dim3 grid((unsigned)((p.workers + per_block - 1) / per_block)), block(32 * (s.warps > 1 ? s.warps : per_block));
+    const int threads = s.lanes > 0 ? s.lanes : 32 * s.warps;
+    const size_t smem = (size_t)sums * g.per_block * threads * s.nv * s.per * 4;
+    const dim3 grid((unsigned)g.blocks), block((unsigned)(g.per_block * threads));
     const bool post = post_w != nullptr;
-    cudaError_t e;
-    if (dt == SBP_BF16) {
-        e = s.warps == 1 ? launch_norm_backward_kernel<__nv_bfloat16, 1, false>(p, layer, post, grid, block, stream)
-            : s.nv == 1  ? launch_norm_backward_kernel<__nv_bfloat16, 1, true>(p, layer, post, grid, block, stream)
-                         : launch_norm_backward_kernel<__nv_bfloat16, 2, true>(p, layer, post, grid, block, stream);
-    } else {
-        e = s.warps == 1 ? (s.nv == 1 ? launch_norm_backward_kernel<float, 1, false>(p, layer, post, grid, block, stream)
-                                      : launch_norm_backward_kernel<float, 2, false>(p, layer, post, grid, block, stream))
-            : s.nv == 2  ? launch_norm_backward_kernel<float, 2, true>(p, layer, post, grid, block, stream)
-                         : launch_norm_backward_kernel<float, 4, true>(p, layer, post, grid, block, stream);
-    }
+    const cudaError_t e = dt == SBP_BF16 ? pick_norm<__nv_bfloat16>(s, p, layer, post, grid, block, smem, stream)
+                                         : pick_norm<float>(s, p, layer, post, grid, block, smem, stream);
     if (e != cudaSuccess || p.want == 0) return e;
     NormReduceParams r = {};
     r.sums = p.sums;
@@ -707,23 +823,25 @@ cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR,
     r.out[1] = dpost_b;
     r.out[2] = dpre_w;
     r.out[3] = dpre_b;
-    r.dgate = dgate;
+    r.out[4] = p.one_gate ? dgate : nullptr;
+    r.dgate = p.one_gate ? nullptr : dgate;
     r.keep_rows = keep_rows;
     r.M_keep_dev = M_keep_dev;
     r.status_word = status_word;
     r.M_keep_cap = M_keep_cap;
     r.workers = p.workers;
-    r.groups = dgate != nullptr ? (M + gate_group - 1) / gate_group : 0;
     r.gate_group = gate_group;
+    r.gate_rows = p.one_gate ? 0 : gate_rows;
     r.C = (int)C;
     r.accumulate = accumulate;
-    auto slices_for = [](int64_t rows) { return rows > 64 ? 32 : rows > 8 ? 8 : 1; };
-    r.slices = slices_for(p.workers);
-    r.gate_slices = r.groups > 0 ? slices_for(p.workers / r.groups) : 1;
-    r.sum_tiles = (int)((C + 256 / r.slices - 1) / (256 / r.slices));
-    r.gate_tiles = (int)((C + 256 / r.gate_slices - 1) / (256 / r.gate_slices));
-    const int64_t blocks = (int64_t)kNormSums * r.sum_tiles + r.groups * r.gate_tiles;
-    return launch_pdl(norm_reduce_kernel, dim3((unsigned)blocks), dim3(256), 0, stream, r);
+    r.blocks = g.blocks;
+    for (int k = 0; k < kNormSums; ++k)
+        if (r.out[k] != nullptr) r.output[r.outputs++] = k;
+    r.few_workers = r.gate_rows > 0 && p.workers / r.gate_rows <= 16;
+    r.tiles = (int)((C + 31) / 32);
+    r.gate_tiles = r.few_workers ? (int)((C + 255) / 256) : r.tiles;
+    const int64_t blocks = (int64_t)r.outputs * r.tiles + (r.few_workers ? (r.gate_rows + 3) / 4 : r.gate_rows) * r.gate_tiles;
+    return launch_pdl(norm_reduce_kernel, dim3((unsigned)blocks), dim3(kReduceThreads), 0, stream, r);
 }
 
 }  // namespace sbp

@@ -44,22 +44,20 @@ embedding_forward_kernel(const uint4* __restrict__ table, const RowLength row, i
     for (int u = 0; u < kCopyUnroll; ++u) {
         const int64_t i = begin + threadIdx.x + u * kCopyThreads;
         v[u] = src[u] >= 0 ? __ldg(table + src[u]) : zero;
-        if constexpr (kAdd) a[u] = i < total ? ld_row(add + i) : zero;
+        if constexpr (kAdd) a[u] = i < total ? __ldcg(add + i) : zero;
     }
 #pragma unroll
     for (int u = 0; u < kCopyUnroll; ++u) {
         const int64_t i = begin + threadIdx.x + u * kCopyThreads;
         if (i >= total) continue;
-        constexpr int N = Vec<T>::N;
-        float f[N], g[N];
+        constexpr int P = Vec<T>::N / 2;
+        f32x2 f[P], g[P];
         Vec<T>::unpack(v[u], f);
         if constexpr (kAdd) Vec<T>::unpack(a[u], g);
+        const f32x2 k = pair(scale, scale);
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-            if constexpr (kAdd) f[e] = src[u] >= 0 ? fmaf(scale, f[e], g[e]) : g[e];
-            else f[e] = src[u] >= 0 ? scale * f[e] : 0.f;
-        }
-        out[i] = Vec<T>::pack(f);
+        for (int e = 0; e < P; ++e) f[e] = kAdd ? fma(k, f[e], g[e]) : mul(k, f[e]);
+        out[i] = src[u] >= 0 ? Vec<T>::pack(f) : kAdd ? a[u] : zero;
     }
 }
 
@@ -263,18 +261,16 @@ struct SumParams {
     float scale;
 };
 
-template <int N>
-__device__ __forceinline__ void put_sum(float* to, const float (&f)[N], float scale, bool add) {
+template <int P>
+__device__ __forceinline__ void put_sum(float* to, const f32x2 (&f)[P], float scale, bool add_old) {
 #pragma unroll
-    for (int e = 0; e < N; e += 4) {
-        float4* q = reinterpret_cast<float4*>(to + e);
-        float4 s = make_float4(scale * f[e], scale * f[e + 1], scale * f[e + 2], scale * f[e + 3]);
-        if (add) {
+    for (int e = 0; e < P; e += 2) {
+        float4* q = reinterpret_cast<float4*>(to + 2 * e);
+        const float2 a = both(f[e]), b = both(f[e + 1]);
+        float4 s = make_float4(scale * a.x, scale * a.y, scale * b.x, scale * b.y);
+        if (add_old) {
             const float4 old = *q;
-            s.x += old.x;
-            s.y += old.y;
-            s.z += old.z;
-            s.w += old.w;
+            s = make_float4(s.x + old.x, s.y + old.y, s.z + old.z, s.w + old.w);
         }
         *q = s;
     }
@@ -284,7 +280,7 @@ __device__ __forceinline__ void put_sum(float* to, const float (&f)[N], float sc
 constexpr int kSumUnroll = 8;
 template <typename T>
 __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumParams p) {
-    constexpr int N = Vec<T>::N;
+    constexpr int N = Vec<T>::N, P = N / 2;
     pdl_launch_dependents();
     pdl_wait();
     const int lane = threadIdx.x & 31;
@@ -299,14 +295,14 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumParams p) {
     const int64_t C = (int64_t)p.vecs * N;
     const uint32_t left = lo > 0 ? p.keys[lo - 1] : 0xffffffffu, right = hi < n ? p.keys[hi] : 0xffffffffu;
     uint32_t cur = p.keys[lo];
-    float acc[N];
+    f32x2 acc[P];
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] = 0.f;
+    for (int e = 0; e < P; ++e) acc[e] = pair(0.f, 0.f);
     auto put = [&](bool last) {
         if (!in) return;
-        if (cur == left) put_sum<N>(p.partial + piece * 2 * C + (int64_t)v * N, acc, 1.f, false);
-        else if (last && cur == right) put_sum<N>(p.partial + (piece * 2 + 1) * C + (int64_t)v * N, acc, 1.f, false);
-        else put_sum<N>(p.dTable + (int64_t)cur * C + (int64_t)v * N, acc, p.scale, p.accumulate != 0);
+        if (cur == left) put_sum(p.partial + piece * 2 * C + (int64_t)v * N, acc, 1.f, false);
+        else if (last && cur == right) put_sum(p.partial + (piece * 2 + 1) * C + (int64_t)v * N, acc, 1.f, false);
+        else put_sum(p.dTable + (int64_t)cur * C + (int64_t)v * N, acc, p.scale, p.accumulate != 0);
     };
     for (int64_t base = lo; base < hi && cur < V; base += 32) {
         const uint32_t my_key = base + lane < hi ? p.keys[base + lane] : V;
@@ -328,12 +324,12 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumParams p) {
                     put(false);
                     cur = k;
 #pragma unroll
-                    for (int e = 0; e < N; ++e) acc[e] = 0.f;
+                    for (int e = 0; e < P; ++e) acc[e] = pair(0.f, 0.f);
                 }
-                float f[N];
+                f32x2 f[P];
                 Vec<T>::unpack(q[u], f);
 #pragma unroll
-                for (int e = 0; e < N; ++e) acc[e] += f[e];
+                for (int e = 0; e < P; ++e) acc[e] = add(acc[e], f[e]);
             }
         }
         if (count < most) {                           // the rest of the list has no ids
@@ -348,8 +344,8 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumParams p) {
 // take the pieces in turns, and their sums are added in the order of the warps.
 template <typename T>
 __global__ void __launch_bounds__(256) embedding_join_kernel(const SumParams p) {
-    constexpr int N = Vec<T>::N;
-    __shared__ float part[8][32][N + 1];
+    constexpr int N = Vec<T>::N, P = N / 2;
+    __shared__ f32x2 part[8][32][P + 1];
     pdl_launch_dependents();
     pdl_wait();
     const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap);
@@ -367,27 +363,27 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumParams p) 
     }
     const int v = (int)(blockIdx.x % p.strips) * 32 + lane;
     const int64_t C = (int64_t)p.vecs * N;
-    float acc[N];
+    f32x2 acc[P];
 #pragma unroll
-    for (int e = 0; e < N; ++e) acc[e] = 0.f;
+    for (int e = 0; e < P; ++e) acc[e] = pair(0.f, 0.f);
     if (v < p.vecs) {
 #pragma unroll 4
         for (int64_t q = piece + warp; q < end; q += 8) {
-            float f[N];
+            f32x2 f[P];
             load_f32<N>(p.partial + (q * 2 + (q == piece ? 1 : 0)) * C + (int64_t)v * N, f);
 #pragma unroll
-            for (int e = 0; e < N; ++e) acc[e] += f[e];
+            for (int e = 0; e < P; ++e) acc[e] = add(acc[e], f[e]);
         }
     }
 #pragma unroll
-    for (int e = 0; e < N; ++e) part[warp][lane][e] = acc[e];
+    for (int e = 0; e < P; ++e) part[warp][lane][e] = acc[e];
     __syncthreads();
     if (warp != 0 || v >= p.vecs) return;
 #pragma unroll
     for (int w = 1; w < 8; ++w)
 #pragma unroll
-        for (int e = 0; e < N; ++e) acc[e] += part[w][lane][e];
-    put_sum<N>(p.dTable + (int64_t)k * C + (int64_t)v * N, acc, p.scale, p.accumulate != 0);
+        for (int e = 0; e < P; ++e) acc[e] = add(acc[e], part[w][lane][e]);
+    put_sum(p.dTable + (int64_t)k * C + (int64_t)v * N, acc, p.scale, p.accumulate != 0);
 }
 
 // ---- host ----

@@ -23,7 +23,6 @@
 // the next.  (One launch a product, seventeen a call, cost 8 us each before their first tile.)  Operands come by TMA, X in either
 // orientation as it lies; tcgen05.mma into accumulators in turns; the epilogue forms the next operand from the sums.  A and B
 // are symmetric: only tiles on and above the diagonal are made, and stored both ways.
-#include "row_math.cuh"
 #include "tc_ptx.cuh"
 
 #include <cuda_fp16.h>

@@ -5,24 +5,50 @@
 
 namespace sbp {
 
+// Two fp32 numbers in a register pair, for the instructions that work on both.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float lo, float hi) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 both(f32x2 v) {
+    float2 f;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(f.x), "=f"(f.y) : "l"(v));
+    return f;
+}
+__device__ __forceinline__ f32x2 add(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 mul(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
+}
+__device__ __forceinline__ f32x2 fma(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+
 template <typename T>
 struct Vec;                                           // T numbers in a 16-byte vector
 template <>
 struct Vec<__nv_bfloat16> {
     static constexpr int N = 8;
-    __device__ static __forceinline__ void unpack(const uint4& q, float* f) {
+    __device__ static __forceinline__ void unpack(const uint4& q, f32x2* f) {
         const uint32_t w[4] = {q.x, q.y, q.z, q.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            f[2 * i] = __uint_as_float(w[i] << 16);
-            f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-        }
+        for (int i = 0; i < 4; ++i) f[i] = pair(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xffff0000u));
     }
-    __device__ static __forceinline__ uint4 pack(const float* f) {
+    __device__ static __forceinline__ uint4 pack(const f32x2* f) {
         uint32_t w[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const __nv_bfloat162 v = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]);
+            const float2 x = both(f[i]);
+            const __nv_bfloat162 v = __floats2bfloat162_rn(x.x, x.y);
             w[i] = *reinterpret_cast<const uint32_t*>(&v);
         }
         return make_uint4(w[0], w[1], w[2], w[3]);
@@ -31,60 +57,85 @@ struct Vec<__nv_bfloat16> {
 template <>
 struct Vec<float> {
     static constexpr int N = 4;
-    __device__ static __forceinline__ void unpack(const uint4& q, float* f) {
-        f[0] = __uint_as_float(q.x);
-        f[1] = __uint_as_float(q.y);
-        f[2] = __uint_as_float(q.z);
-        f[3] = __uint_as_float(q.w);
+    __device__ static __forceinline__ void unpack(const uint4& q, f32x2* f) {
+        f[0] = pair(__uint_as_float(q.x), __uint_as_float(q.y));
+        f[1] = pair(__uint_as_float(q.z), __uint_as_float(q.w));
     }
-    __device__ static __forceinline__ uint4 pack(const float* f) {
-        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    __device__ static __forceinline__ uint4 pack(const f32x2* f) {
+        const float2 a = both(f[0]), b = both(f[1]);
+        return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
     }
 };
 
 // N consecutive fp32 numbers (a multiple of four, 16-byte aligned) that no kernel writes meanwhile
 template <int N>
-__device__ __forceinline__ void load_f32(const float* p, float* f) {
+__device__ __forceinline__ void load_f32(const float* p, f32x2* f) {
 #pragma unroll
-    for (int i = 0; i < N; i += 4) {
-        const float4 v = __ldg(reinterpret_cast<const float4*>(p + i));
-        f[i] = v.x;
-        f[i + 1] = v.y;
-        f[i + 2] = v.z;
-        f[i + 3] = v.w;
-    }
+    for (int i = 0; i < N / 4; ++i) Vec<float>::unpack(__ldg(reinterpret_cast<const uint4*>(p) + i), f + 2 * i);
 }
 
-// a row that is read once; not through the read-only path, for the buffer may be written in place by the same thread
-__device__ __forceinline__ uint4 ld_row(const uint4* p) {
-    uint4 v;
-    asm volatile("ld.global.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p) : "memory");
-    return v;
-}
+// The threads that share a row: kLanes (8, 16 or 32) of a warp, or, kLanes 0, `warps` warps of a block, which meet at barrier `id`
+// and add up through `scratch`: two halves of a float4 a warp, taken in turns - a half is written again only after the barrier of
+// the sum between, by which every thread has read it.
+template <int kLanes>
+struct RowThreads {
+    static constexpr bool kMulti = kLanes == 0;
+    int t, count;                                     // this thread, of how many
+    int warps, id, turn;
+    float4* scratch;
+    __device__ __forceinline__ int threads() const { return kMulti ? count : kLanes; }
 
-// Sums of V values over a row's threads: one warp, or all the warps of a block (kMulti), through shared memory.  `scratch` holds
-// two halves of V floats a warp, taken in turns: a half is written again only after the barrier of the sum between, by which
-// every thread has read it.  The order of additions depends on the number of threads alone.
-template <int V, bool kMulti>
-__device__ __forceinline__ void row_sums(float (&v)[V], float* scratch, int warps, int& turn) {
+    // Sums of V <= 4 values over those threads, in an order that depends on their number alone.  Several values over 32 lanes take
+    // six exchanges: each of the first two halves what a lane carries.
+    template <int V>
+    __device__ __forceinline__ void sums(float (&v)[V]) {
+        const int lane = threadIdx.x & 31;
+        if constexpr (V == 1 || (!kMulti && kLanes < 32)) {
 #pragma unroll
-    for (int o = 16; o > 0; o >>= 1)
+            for (int o = (kMulti ? 32 : kLanes) / 2; o > 0; o >>= 1)
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
-    if constexpr (kMulti) {
-        float* s = scratch + (turn ? 32 * V : 0);
-        turn ^= 1;
-        if ((threadIdx.x & 31) == 0) {
-#pragma unroll
-            for (int i = 0; i < V; ++i) s[(threadIdx.x >> 5) * V + i] = v[i];
+                for (int i = 0; i < V; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
+            if constexpr (!kMulti) return;
         }
-        __syncthreads();
+        float s = v[0];
+        if constexpr (V > 1) {                        // lanes 8 k .. 8 k + 7 come to hold the sum of value k
+            const bool h4 = lane & 16, h3 = lane & 8;
+            const float v2 = V > 2 ? v[V > 2 ? 2 : 0] : 0.f, v3 = V > 3 ? v[V > 3 ? 3 : 0] : 0.f;
+            float a = h4 ? v2 : v[0], b = h4 ? v3 : v[1];
+            a += __shfl_xor_sync(0xffffffffu, h4 ? v[0] : v2, 16);
+            b += __shfl_xor_sync(0xffffffffu, h4 ? v[1] : v3, 16);
+            s = h3 ? b : a;
+            s += __shfl_xor_sync(0xffffffffu, h3 ? a : b, 8);
+            s += __shfl_xor_sync(0xffffffffu, s, 4);
+            s += __shfl_xor_sync(0xffffffffu, s, 2);
+            s += __shfl_xor_sync(0xffffffffu, s, 1);
+        }
+        if constexpr (!kMulti) {
 #pragma unroll
-        for (int i = 0; i < V; ++i) v[i] = 0.f;
-        for (int w = 0; w < warps; ++w)
-#pragma unroll
-            for (int i = 0; i < V; ++i) v[i] += s[w * V + i];
+            for (int i = 0; i < V; ++i) v[i] = __shfl_sync(0xffffffffu, s, 8 * i);
+        } else {
+            float4* half = scratch + (turn ? 16 : 0);
+            turn ^= 1;
+            if ((lane & 7) == 0) reinterpret_cast<float*>(half + (t >> 5))[lane >> 3] = s;     // (V == 1: the sum four times)
+            asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
+            float4 f = half[0];
+            auto more = [&](int w) {
+                const float4 q = half[w];
+                f.x += q.x;
+                if constexpr (V > 1) f.y += q.y;
+                if constexpr (V > 2) f.z += q.z;
+                if constexpr (V > 3) f.w += q.w;
+            };
+            if (warps > 1) more(1);
+            if (warps > 2) more(2);
+            if (warps > 3) more(3);
+            for (int w = 4; w < warps; ++w) more(w);
+            v[0] = f.x;
+            if constexpr (V > 1) v[1] = f.y;
+            if constexpr (V > 2) v[2] = f.z;
+            if constexpr (V > 3) v[3] = f.w;
+        }
     }
-}
+};
 
 }  // namespace sbp

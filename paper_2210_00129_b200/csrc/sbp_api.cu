@@ -402,7 +402,7 @@ sbp_status sbp_block_norm_forward(sbp_dtype dt, sbp_norm norm, const void* H, co
 
 size_t sbp_block_norm_backward_workspace_bytes(sbp_dtype dt, int64_t M, int64_t M_keep_cap, int64_t C) {
     if ((dt != SBP_F32 && dt != SBP_BF16) || M <= 0 || M_keep_cap < 0 || M_keep_cap > M || C <= 0 || C > block_norm_max_channels()) return 256;
-    return align_up(block_norm_backward_workspace_bytes(dt, M_keep_cap, C), 256);
+    return align_up(block_norm_backward_workspace_bytes(dt, M, M_keep_cap, C), 256);
 }
 
 sbp_status sbp_block_norm_backward(sbp_dtype dt, sbp_norm norm, const void* dR, const void* dZ, const void* R_keep, const void* Y_keep,

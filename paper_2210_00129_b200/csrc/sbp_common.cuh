@@ -213,7 +213,7 @@ cudaError_t launch_block_norm_forward(sbp_dtype dt, bool layer, const void* H, c
                                       int64_t M, int64_t C, void* R, void* Z, const int32_t* keep_rows, const int32_t* M_keep_dev,
                                       int64_t M_keep_cap, void* Y_keep, void* R_keep, void* Z_keep, const int32_t* status_word,
                                       cudaStream_t stream);
-size_t block_norm_backward_workspace_bytes(sbp_dtype dt, int64_t M_keep_cap, int64_t C);
+size_t block_norm_backward_workspace_bytes(sbp_dtype dt, int64_t M, int64_t M_keep_cap, int64_t C);
 cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR, const void* dZ, const void* R_keep, const void* Y_keep,
                                        const float* post_w, const float* post_b, const void* gate, int64_t gate_group, float scale,
                                        const float* pre_w, float eps, const int32_t* keep_rows, const int32_t* M_keep_dev, int64_t M,
