@@ -45,7 +45,7 @@ norm_forward_kernel(const NormFwdParams p) {
     constexpr int VN = Vec<T>::N, P = VN / 2, E2 = kNV * P;          // pairs of a vector, pairs a thread holds of a row
     constexpr int kU = E2 > 4 ? 1 : 2;
     constexpr int kGroups = kMulti ? 1 : 32 / (kMulti ? 32 : kLanes);
-    __shared__ float4 scratch[kMulti ? 32 : 1];
+    __shared__ float4 scratch[kMulti ? 64 : 1];
     pdl_launch_dependents();
     pdl_wait();
     if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
@@ -233,285 +233,339 @@ struct NormBwdParams {
     int want;                                         // bit k: sum k is wanted
     int one_gate;                                     // the gate has one row: its gradient is a sum like the others
     int vecs, warps, per_block, accumulate, copy_rest;               // warps of a worker (kLanes 0), workers of a block
+    int blocks;                                       // with workers; those behind them only copy
     float scale, eps, inv_c;
 };
 
 __device__ __forceinline__ int64_t norm_chunk(int64_t M_keep, int64_t workers) { return (M_keep + workers - 1) / workers; }
 
-// Threads of a block, one block an SM: registers for rows of 8 numbers a thread, or of more.
-__host__ __device__ constexpr int norm_backward_threads(int numbers) { return numbers <= 8 ? 768 : 512; }
+// Rows that a worker has at a time, and threads of a block (one an SM), by the numbers a thread has of a row: two rows share what a row
+// costs besides its numbers, and give a warp something to do while it waits for the sums of either.
+__host__ __device__ constexpr int norm_backward_rows(int numbers, bool many_warps) { return numbers <= 8 && !many_warps ? 2 : 1; }
+__host__ __device__ constexpr int norm_backward_threads(int numbers, bool many_warps) { return numbers <= 8 && !many_warps ? 384 : 512; }
 
-// A worker - kLanes threads of a warp, or, kLanes 0, some warps - takes consecutive kept rows; a thread has the same kNV vectors of
-// each.  The weights' gradients are sums over rows: a worker's lie in shared memory, four numbers a thread and place, which only
-// that thread touches (five sums of 24 channels a thread do not fit in registers beside the row); at the end the block's workers are
-// added up and the block leaves one partial row for a second launch.  A warp has a whole row up to 1024 bf16 or 512 fp32 channels, so
-// that its sums need no barrier, and rows of few channels go several to a warp: what a row costs besides its numbers - three
-// rounds of sums over its threads, addresses, the gate row - was most of the instructions with one vector a thread.
-// The gate's gradient is a sum over the rows of one gate row; the list is ascending, so a gate row's rows are consecutive: the sum
-// is put away when the gate row changes - straight into dgate where no other worker has rows of it (all but a worker's first
-// and last gate row).
-template <typename T, int kNV, int kLanes, bool kFull, bool kLayer, bool kPost>
-__global__ void __launch_bounds__(norm_backward_threads(kNV * Vec<T>::N), 1) norm_backward_kernel(const NormBwdParams p) {
+// A worker - kLanes threads of a warp, or, kLanes 0, some warps - takes consecutive kept rows, two at a time where they fit in the
+// registers; a thread has the same kNV vectors of each, so that its share of the weights' gradients stays there too: the sums of
+// dZ n_R and dZ, and, for the rows of one gate row, S1 = sum G n_Y and S0 = sum G, of which the other three are made when the gate
+// row changes (dgate = post_w S1 + post_b S0, dpost_w += gate S1, dpost_b += gate S0).  At the end the block's workers are added up
+// in shared memory, and the block leaves one partial row of each sum for a second launch.
+// The list is ascending, so a gate row's rows are consecutive; dgate leaves a row at a time - straight to its place where no other
+// worker has rows of it (all but a worker's first and last gate row).
+// Every instruction besides the arithmetic counts here: with the five sums in shared memory, read and written for every row, the
+// shared memory was the bound (25088 x 768: 62 us; in registers, one row at a time, 67).
+template <typename T, int kNV, int kLanes, bool kMany, bool kFull, bool kLayer, bool kPost>
+__global__ void __launch_bounds__(norm_backward_threads(kNV * Vec<T>::N, kMany), 1) norm_backward_kernel(const NormBwdParams p) {
     constexpr bool kMulti = kLanes == 0;
     constexpr int VN = Vec<T>::N, P = VN / 2, E2 = kNV * P, kQ = VN / 4;      // kQ: float4 of a vector's sums
+    constexpr int kU = norm_backward_rows(kNV * VN, kMany);
     extern __shared__ float4 sums_s[];                // [worker of the block][wanted sum][vector of the thread][kQ][thread]
-    __shared__ float4 scratch[kMulti ? kNormMostWorkers * 32 : 1];
+    __shared__ float4 scratch[kMulti ? (kMany ? 1 : kNormMostWorkers) * 64 : 1];
     pdl_launch_dependents();
     pdl_wait();
     if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int width = kMulti ? p.warps * 32 : kLanes, mine = threadIdx.x / width;          // threads of a worker; which one of the block
-    RowThreads<kLanes> row = {(int)threadIdx.x % width, width, p.warps, mine + 1, 0, scratch + mine * 32};
+    RowThreads<kLanes> row = {(int)threadIdx.x % width, width, p.warps, mine + 1, 0, scratch + mine * 64};
     const int t = row.t, threads = row.threads();
     const int64_t worker = (int64_t)blockIdx.x * p.per_block + mine;
     const int64_t M_keep = load_m_keep(p.M_keep_dev, p.M_keep_cap);
-    const int64_t chunk = norm_chunk(M_keep, p.workers);
-    const int64_t lo = worker * chunk < M_keep ? worker * chunk : M_keep, hi = lo + chunk < M_keep ? lo + chunk : M_keep;
-    const int64_t C = (int64_t)p.vecs * VN;
     const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
-    const int per_sum = kNV * kQ * threads, wanted = __popc(p.want);
-    float4* own = sums_s + (int64_t)mine * wanted * per_sum + t;
-    float4* place[kNormSums];                         // of the wanted sums
+    if (blockIdx.x < (unsigned)p.blocks) {
+        const int64_t chunk = norm_chunk(M_keep, p.workers);
+        const int64_t lo = worker * chunk < M_keep ? worker * chunk : M_keep, hi = lo + chunk < M_keep ? lo + chunk : M_keep;
+        const int64_t C = (int64_t)p.vecs * VN;
+        const int per_sum = kNV * kQ * threads, wanted = __popc(p.want);
+        float4* own = sums_s + (int64_t)mine * wanted * per_sum + t;
+        auto place = [&](int k) { return own + __popc(p.want & ((1 << k) - 1)) * per_sum; };   // of a wanted sum
+        for (int i = 0; i < wanted * kNV * kQ; ++i) own[i * threads] = make_float4(0.f, 0.f, 0.f, 0.f);
+        bool in[kNV];
 #pragma unroll
-    for (int k = 0; k < kNormSums; ++k) place[k] = own + __popc(p.want & ((1 << k) - 1)) * per_sum;
-    for (int i = 0; i < wanted * kNV * kQ; ++i) own[i * threads] = make_float4(0.f, 0.f, 0.f, 0.f);
-    bool in[kNV];
+        for (int j = 0; j < kNV; ++j) in[j] = kFull || t + j * threads < p.vecs;
+        const f32x2 none = pair(0.f, 0.f);
+        f32x2 pre1[E2], pre0[E2], S1[E2], S0[E2];
 #pragma unroll
-    for (int j = 0; j < kNV; ++j) in[j] = kFull || t + j * threads < p.vecs;
-    auto accumulate = [&](float4* sum, int j, const f32x2* f) {
-#pragma unroll
-        for (int h = 0; h < kQ; ++h) {
-            float4* a = sum + (j * kQ + h) * threads;
-            const float4 old = *a;
-            const float2 u = both(add(pair(old.x, old.y), f[2 * h])), v = both(add(pair(old.z, old.w), f[2 * h + 1]));
-            *a = make_float4(u.x, u.y, v.x, v.y);
+        for (int e = 0; e < E2; ++e) pre1[e] = pre0[e] = S1[e] = S0[e] = none;
+        uint32_t first = 0, last = 0, cur = 0;
+        if (p.gate != nullptr && lo < hi) {
+            first = cur = p.gate_group((uint32_t)mapped_row(p.keep_rows, lo) & 0x7fffffffu);
+            last = p.gate_group((uint32_t)mapped_row(p.keep_rows, hi - 1) & 0x7fffffffu);
         }
-    };
-    const bool gate_rows = (p.want & 16) && !p.one_gate;
-    uint32_t first = 0, last = 0, cur = 0;
-    if (p.gate != nullptr && lo < hi) {
-        first = cur = p.gate_group((uint32_t)mapped_row(p.keep_rows, lo) & 0x7fffffffu);
-        last = p.gate_group((uint32_t)mapped_row(p.keep_rows, hi - 1) & 0x7fffffffu);
-    }
-    auto put_gate = [&]() {                           // the gate row's sum, out of shared memory
-        const bool partial = cur == first || cur == last;
-        float* to = partial ? p.gate_sums + (worker * 2 + (cur == first ? 0 : 1)) * C : p.dgate + (int64_t)cur * C;
-#pragma unroll
-        for (int j = 0; j < kNV; ++j) {
-            if (!in[j]) continue;
-#pragma unroll
-            for (int h = 0; h < kQ; ++h) {
-                float4* a = place[4] + (j * kQ + h) * threads;
-                float4 s = *a;
-                *a = make_float4(0.f, 0.f, 0.f, 0.f);
-                float4* q = reinterpret_cast<float4*>(to + (int64_t)(t + j * threads) * VN) + h;
-                if (!partial && p.accumulate) {
-                    const float4 old = *q;
-                    s = make_float4(s.x + old.x, s.y + old.y, s.z + old.z, s.w + old.w);
-                }
-                *q = s;
-            }
-        }
-    };
-    auto total = [](f32x2 a) { return both(a).x + both(a).y; };
-    // (several rows a warp: every group of lanes goes round as often as the others, with nothing to do behind its last row)
-    constexpr bool kSplit = !kMulti && kLanes < 32;
-    const int rounds = kSplit ? (int)chunk : (int)(hi - lo);
-    int32_t next = lo < hi ? mapped_row(p.keep_rows, lo) : -1;
-    int64_t at = lo * p.vecs + t;
-    for (int i = 0; i < rounds; ++i, at += p.vecs) {
-        const bool have = !kSplit || lo + i < hi;
-        const int32_t k = next;
-        const bool live = have && k >= 0 && k < p.M;
-        next = lo + i + 1 < hi ? mapped_row(p.keep_rows, lo + i + 1) : -1;
-        if (!kSplit && !live) {                       // an entry outside the tensor is skipped
-            if (p.dY != nullptr) {
-#pragma unroll
-                for (int j = 0; j < kNV; ++j)
-                    if (in[j]) p.dY[at + j * threads] = zero;
-            }
-            continue;
-        }
-        const int64_t full = (int64_t)k * p.vecs + t;
-        f32x2 x[E2], y[E2], g[E2], q[E2];              // R, then what its norm makes of it; Y likewise; dZ; dZ pre_w
-        uint4 dq[kNV];
-        {
-            uint4 rq[kNV], yq[kNV], zq[kNV];
+        auto accumulate = [&](float4* a, const f32x2* f, bool old) {     // into shared memory (old: or a row of memory)
+            const float2 u = both(f[0]), v = both(f[1]);
+            float4 s = make_float4(u.x, u.y, v.x, v.y);
+            if (old) s = make_float4(s.x + a->x, s.y + a->y, s.z + a->z, s.w + a->w);
+            *a = s;
+        };
+        auto put_gate = [&]() {                           // the end of a gate row (or, without a gate, of the list): S1 and S0 go where they belong
+            const bool partial = cur == first || cur == last;
+            float* to = partial ? p.gate_sums + (worker * 2 + (cur == first ? 0 : 1)) * C : p.dgate + (int64_t)cur * C;
 #pragma unroll
             for (int j = 0; j < kNV; ++j) {
-                const bool ok = in[j] && live;
-                rq[j] = ok && p.dZ != nullptr ? __ldcg(p.R_keep + at + j * threads) : zero;
-                zq[j] = ok && p.dZ != nullptr ? __ldcg(p.dZ + at + j * threads) : zero;
-                yq[j] = ok && p.Y_keep != nullptr ? __ldcg(p.Y_keep + at + j * threads) : zero;
-                dq[j] = ok && p.dR != nullptr ? __ldcg(p.dR + full + j * threads) : zero;
+                if (!in[j]) continue;
+                const int v = t + j * threads;
+                f32x2 f[P], w[P];
+                if (p.want & 16) {
+#pragma unroll
+                    for (int e = 0; e < P; ++e) f[e] = S1[j * P + e];
+                    if constexpr (kPost) {
+                        load_f32<VN>(p.post_w + v * VN, w);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) f[e] = mul(f[e], w[e]);
+                        if (p.post_b != nullptr) {
+                            load_f32<VN>(p.post_b + v * VN, w);
+#pragma unroll
+                            for (int e = 0; e < P; ++e) f[e] = fma(S0[j * P + e], w[e], f[e]);
+                        }
+                    }
+#pragma unroll
+                    for (int h = 0; h < kQ; ++h) {
+                        if (p.one_gate) accumulate(place(4) + (j * kQ + h) * threads, f + 2 * h, true);
+                        else accumulate(reinterpret_cast<float4*>(to + (int64_t)v * VN) + h, f + 2 * h, !partial && p.accumulate);
+                    }
+                }
+                if constexpr (kPost) {
+#pragma unroll
+                    for (int e = 0; e < P; ++e) w[e] = pair(1.f, 1.f);
+                    if (p.gate != nullptr) Vec<T>::unpack(__ldg(p.gate + (int64_t)cur * p.vecs + v), w);
+                    auto add_to = [&](int k, const f32x2* s) {
+#pragma unroll
+                        for (int e = 0; e < P; ++e) f[e] = mul(s[e], w[e]);
+#pragma unroll
+                        for (int h = 0; h < kQ; ++h) accumulate(place(k) + (j * kQ + h) * threads, f + 2 * h, true);
+                    };
+                    if (p.want & 1) add_to(0, &S1[j * P]);
+                    if (p.want & 2) add_to(1, &S0[j * P]);
+                }
+            }
+#pragma unroll
+            for (int e = 0; e < E2; ++e) S1[e] = S0[e] = none;
+        };
+        auto total = [](f32x2 a) { return both(a).x + both(a).y; };
+        // (several rows a warp: every group of lanes goes round as often as the others, with nothing to do behind its last row)
+        constexpr bool kSplit = !kMulti && kLanes < 32;
+        const int rounds = kSplit ? (int)chunk : (int)(hi - lo);
+        int64_t at = lo * p.vecs + t;
+        auto ids = [&](int i, int32_t (&k)[kU]) {         // (-1: no row, or an entry outside the tensor, which is skipped)
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                k[u] = lo + i + u < hi ? mapped_row(p.keep_rows, lo + i + u) : -1;
+                if (k[u] >= p.M) k[u] = -1;
+            }
+        };
+        int32_t next[kU];
+        ids(0, next);
+        for (int i = 0; i < rounds; i += kU, at += kU * (int64_t)p.vecs) {
+            int32_t k[kU];
+            bool have[kU], live[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                k[u] = next[u];
+                have[u] = lo + i + u < hi;
+                live[u] = k[u] >= 0;
+            }
+            f32x2 x[kU][E2], y[kU][E2], g[kU][E2], q[kU][E2];            // R, then what its norm makes of it; Y likewise; dZ; dZ pre_w
+            uint4 dq[kU][kNV];
+            ids(i + kU, next);
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                uint4 rq[kNV], yq[kNV], zq[kNV];
+#pragma unroll
+                for (int j = 0; j < kNV; ++j) {
+                    const int64_t from = at + (int64_t)u * p.vecs + j * threads;
+                    const bool ok = in[j] && have[u];
+                    rq[j] = ok && p.dZ != nullptr ? __ldcg(p.R_keep + from) : zero;
+                    zq[j] = ok && p.dZ != nullptr ? __ldcg(p.dZ + from) : zero;
+                    yq[j] = ok && p.Y_keep != nullptr ? __ldcg(p.Y_keep + from) : zero;
+                    dq[u][j] = in[j] && live[u] && p.dR != nullptr ? __ldcg(p.dR + (int64_t)k[u] * p.vecs + t + j * threads) : zero;
+                }
+#pragma unroll
+                for (int j = 0; j < kNV; ++j) {
+                    Vec<T>::unpack(rq[j], &x[u][j * P]);
+                    Vec<T>::unpack(yq[j], &y[u][j * P]);
+                    Vec<T>::unpack(zq[j], &g[u][j * P]);
+                }
             }
 #pragma unroll
             for (int j = 0; j < kNV; ++j) {
                 f32x2 w[P];
 #pragma unroll
-                for (int e = 0; e < P; ++e) w[e] = pair(0.f, 0.f);
+                for (int e = 0; e < P; ++e) w[e] = none;
                 if (in[j] && p.dZ != nullptr) load_f32<VN>(p.pre_w + (t + j * threads) * VN, w);
-                Vec<T>::unpack(rq[j], &x[j * P]);
-                Vec<T>::unpack(yq[j], &y[j * P]);
-                Vec<T>::unpack(zq[j], &g[j * P]);
 #pragma unroll
-                for (int e = 0; e < P; ++e) q[j * P + e] = mul(g[j * P + e], w[e]);
+                for (int u = 0; u < kU; ++u)
+#pragma unroll
+                    for (int e = 0; e < P; ++e) q[u][j * P + e] = mul(g[u][j * P + e], w[e]);
             }
-        }
-        float s1[3] = {0.f, 0.f, 0.f}, s2[3];
-        if constexpr (kLayer) {
-            f32x2 sx = x[0], sy = y[0], sq = q[0];
+            float s1[3 * kU], s2[3 * kU];
+            if constexpr (kLayer) {
 #pragma unroll
-            for (int e = 1; e < E2; ++e) {
-                sx = add(sx, x[e]);
-                if constexpr (kPost) sy = add(sy, y[e]);
-                sq = add(sq, q[e]);
-            }
-            s1[0] = total(sx);
-            s1[1] = kPost ? total(sy) : 0.f;
-            s1[2] = total(sq);
-            row.sums(s1);
+                for (int u = 0; u < kU; ++u) {
+                    f32x2 sx = x[u][0], sy = y[u][0], sq = q[u][0];
 #pragma unroll
-            for (int j = 0; j < kNV; ++j) {
-                const float mx = in[j] ? -s1[0] * p.inv_c : 0.f, my = in[j] ? -s1[1] * p.inv_c : 0.f;       // threads past the row keep zeros
-#pragma unroll
-                for (int e = j * P; e < (j + 1) * P; ++e) {
-                    x[e] = add(x[e], pair(mx, mx));
-                    if constexpr (kPost) y[e] = add(y[e], pair(my, my));
-                }
-            }
-        }
-        {
-            f32x2 sx = mul(x[0], x[0]), sy = mul(y[0], y[0]), sq = mul(q[0], x[0]);
-#pragma unroll
-            for (int e = 1; e < E2; ++e) {
-                sx = fma(x[e], x[e], sx);
-                if constexpr (kPost) sy = fma(y[e], y[e], sy);
-                sq = fma(q[e], x[e], sq);
-            }
-            s2[0] = total(sx);
-            s2[1] = kPost ? total(sy) : 0.f;
-            s2[2] = total(sq);
-            row.sums(s2);
-        }
-        const float rstd = rsqrtf(fmaf(s2[0], p.inv_c, p.eps)), rstd_y = kPost ? rsqrtf(fmaf(s2[1], p.inv_c, p.eps)) : 1.f;
-        // d + rstd (q - mean(q) - n mean(q n)), n = rstd x
-        const float k0 = kLayer ? -s1[2] * p.inv_c * rstd : 0.f, k1 = -(s2[2] * p.inv_c * rstd) * rstd;
-        if (live && p.gate != nullptr) {
-            const uint32_t group = p.gate_group((uint32_t)k);
-            if (group != cur) {
-                if (gate_rows) put_gate();
-                cur = group;
-            }
-        }
-        f32x2 sq = pair(0.f, 0.f), sqn = pair(0.f, 0.f);
-        if (live) {
-            const f32x2 rr = pair(rstd, rstd);
-#pragma unroll
-            for (int j = 0; j < kNV; ++j) {
-                if (!in[j]) continue;
-                f32x2 out[P], d[P], w[P], b[P];
-                Vec<T>::unpack(dq[j], d);
-                if (p.dZ != nullptr) {
-#pragma unroll
-                    for (int e = 0; e < P; ++e) {
-                        const f32x2 n = mul(x[j * P + e], rr);
-                        d[e] = add(d[e], fma(q[j * P + e], rr, fma(n, pair(k1, k1), pair(k0, k0))));        // the whole gradient of R
-                        out[e] = mul(g[j * P + e], n);
+                    for (int e = 1; e < E2; ++e) {
+                        sx = add(sx, x[u][e]);
+                        if constexpr (kPost) sy = add(sy, y[u][e]);
+                        sq = add(sq, q[u][e]);
                     }
-                    if (p.want & 4) accumulate(place[2], j, out);
-                    if (p.want & 8) accumulate(place[3], j, &g[j * P]);
+                    s1[3 * u] = total(sx);
+                    s1[3 * u + 1] = kPost ? total(sy) : 0.f;
+                    s1[3 * u + 2] = total(sq);
                 }
-                if (p.dH != nullptr) {
+                row.sums(s1);
 #pragma unroll
-                    for (int e = 0; e < P; ++e) out[e] = mul(d[e], pair(p.scale, p.scale));
-                    p.dH[full + j * threads] = Vec<T>::pack(out);
-                }
-                if constexpr (kPost) {
-                    load_f32<VN>(p.post_w + (t + j * threads) * VN, w);
+                for (int u = 0; u < kU; ++u)
 #pragma unroll
-                    for (int e = 0; e < P; ++e) y[j * P + e] = mul(y[j * P + e], pair(rstd_y, rstd_y));
+                    for (int j = 0; j < kNV; ++j) {
+                        const float mx = in[j] ? -s1[3 * u] * p.inv_c : 0.f, my = in[j] ? -s1[3 * u + 1] * p.inv_c : 0.f;   // (threads past the row keep zeros)
+#pragma unroll
+                        for (int e = j * P; e < (j + 1) * P; ++e) {
+                            x[u][e] = add(x[u][e], pair(mx, mx));
+                            if constexpr (kPost) y[u][e] = add(y[u][e], pair(my, my));
+                        }
+                    }
+            }
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                f32x2 sx = mul(x[u][0], x[u][0]), sy = mul(y[u][0], y[u][0]), sq = mul(q[u][0], x[u][0]);
+#pragma unroll
+                for (int e = 1; e < E2; ++e) {
+                    sx = fma(x[u][e], x[u][e], sx);
+                    if constexpr (kPost) sy = fma(y[u][e], y[u][e], sy);
+                    sq = fma(q[u][e], x[u][e], sq);
                 }
+                s2[3 * u] = total(sx);
+                s2[3 * u + 1] = kPost ? total(sy) : 0.f;
+                s2[3 * u + 2] = total(sq);
+            }
+            row.sums(s2);
+            float s3[2 * kU], rstd_y[kU];
+#pragma unroll
+            for (int u = 0; u < kU; ++u) {
+                s3[2 * u] = s3[2 * u + 1] = 0.f;
+                const float rstd = rsqrtf(fmaf(s2[3 * u], p.inv_c, p.eps));
+                rstd_y[u] = kPost ? rsqrtf(fmaf(s2[3 * u + 1], p.inv_c, p.eps)) : 1.f;
+                if (!live[u]) continue;
+                // d + rstd (q - mean(q) - n mean(q n)), n = rstd x
+                const float k0 = kLayer ? -s1[3 * u + 2] * p.inv_c * rstd : 0.f, k1 = -(s2[3 * u + 2] * p.inv_c * rstd) * rstd;
                 if (p.gate != nullptr) {
-                    if (p.want & 16) {
-                        if constexpr (kPost)
-                            if (p.post_b != nullptr) load_f32<VN>(p.post_b + (t + j * threads) * VN, b);
+                    const uint32_t group = p.gate_group((uint32_t)k[u]);
+                    if (group != cur) {
+                        put_gate();
+                        cur = group;
+                    }
+                }
+                f32x2 sq = none, sqn = none;
+                const f32x2 rr = pair(rstd, rstd);
+#pragma unroll
+                for (int j = 0; j < kNV; ++j) {
+                    if (!in[j]) continue;
+                    f32x2 out[P], d[P], w[P];
+                    Vec<T>::unpack(dq[u][j], d);
+                    if (p.dZ != nullptr) {
 #pragma unroll
                         for (int e = 0; e < P; ++e) {
-                            f32x2 u = y[j * P + e];
-                            if constexpr (kPost) u = p.post_b != nullptr ? fma(u, w[e], b[e]) : mul(u, w[e]);
-                            out[e] = mul(d[e], u);
+                            const int c = j * P + e;
+                            const f32x2 n = mul(x[u][c], rr);
+                            d[e] = add(d[e], fma(q[u][c], rr, fma(n, pair(k1, k1), pair(k0, k0))));     // the whole gradient of R
+                            pre1[c] = fma(g[u][c], n, pre1[c]);
+                            pre0[c] = add(pre0[c], g[u][c]);
                         }
-                        accumulate(place[4], j, out);
                     }
-                    Vec<T>::unpack(__ldg(p.gate + (int64_t)cur * p.vecs + t + j * threads), b);
+                    if (p.dH != nullptr) {
 #pragma unroll
-                    for (int e = 0; e < P; ++e) d[e] = mul(d[e], b[e]);
-                }
-                if constexpr (kPost) {
-                    if (p.want & 1) {
-#pragma unroll
-                        for (int e = 0; e < P; ++e) out[e] = mul(d[e], y[j * P + e]);
-                        accumulate(place[0], j, out);
+                        for (int e = 0; e < P; ++e) out[e] = mul(d[e], pair(p.scale, p.scale));
+                        p.dH[(int64_t)k[u] * p.vecs + t + j * threads] = Vec<T>::pack(out);
                     }
-                    if (p.want & 2) accumulate(place[1], j, d);
 #pragma unroll
                     for (int e = 0; e < P; ++e) {
-                        d[e] = mul(d[e], w[e]);
-                        sq = add(sq, d[e]);
-                        sqn = fma(d[e], y[j * P + e], sqn);
+                        const int c = j * P + e;
+                        if constexpr (kPost) y[u][c] = mul(y[u][c], pair(rstd_y[u], rstd_y[u]));
+                        S1[c] = fma(d[e], y[u][c], S1[c]);
+                        S0[c] = add(S0[c], d[e]);
+                    }
+                    if (p.gate != nullptr) {
+                        Vec<T>::unpack(__ldg(p.gate + (int64_t)cur * p.vecs + t + j * threads), w);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) d[e] = mul(d[e], w[e]);
+                    }
+                    if constexpr (kPost) {
+                        load_f32<VN>(p.post_w + (t + j * threads) * VN, w);
+#pragma unroll
+                        for (int e = 0; e < P; ++e) {
+                            d[e] = mul(d[e], w[e]);
+                            sq = add(sq, d[e]);
+                            sqn = fma(d[e], y[u][j * P + e], sqn);
+                        }
+                    }
+#pragma unroll
+                    for (int e = 0; e < P; ++e) g[u][j * P + e] = d[e];
+                }
+                s3[2 * u] = total(sq);
+                s3[2 * u + 1] = total(sqn);
+            }
+            if constexpr (kPost) {
+                __syncwarp();
+                row.sums(s3);
+            }
+            if (p.dY != nullptr) {
+#pragma unroll
+                for (int u = 0; u < kU; ++u) {
+                    if (!have[u]) continue;
+                    const float c0 = kLayer ? -s3[2 * u] * p.inv_c * rstd_y[u] : 0.f, c1 = -s3[2 * u + 1] * p.inv_c * rstd_y[u];
+#pragma unroll
+                    for (int j = 0; j < kNV; ++j) {
+                        if (!in[j]) continue;
+                        if constexpr (kPost) {
+#pragma unroll
+                            for (int e = j * P; e < (j + 1) * P; ++e)
+                                g[u][e] = fma(g[u][e], pair(rstd_y[u], rstd_y[u]), fma(y[u][e], pair(c1, c1), pair(c0, c0)));
+                        }
+                        p.dY[at + (int64_t)u * p.vecs + j * threads] = live[u] ? Vec<T>::pack(&g[u][j * P]) : zero;
                     }
                 }
-#pragma unroll
-                for (int e = 0; e < P; ++e) g[j * P + e] = d[e];
             }
+            __syncwarp();
         }
-        if constexpr (kSplit) __syncwarp();
-        float s3[2] = {total(sq), total(sqn)};
-        if constexpr (kPost) row.sums(s3);
-        if (p.dY != nullptr && have) {
-            const float c0 = kLayer ? -s3[0] * p.inv_c * rstd_y : 0.f, c1 = -s3[1] * p.inv_c * rstd_y;
+        if (lo < hi) put_gate();
 #pragma unroll
-            for (int j = 0; j < kNV; ++j) {
-                if (!in[j]) continue;
-                if constexpr (kPost) {
+        for (int j = 0; j < kNV; ++j)
 #pragma unroll
-                    for (int e = j * P; e < (j + 1) * P; ++e) g[e] = fma(g[e], pair(rstd_y, rstd_y), fma(y[e], pair(c1, c1), pair(c0, c0)));
-                }
-                p.dY[at + j * threads] = live ? Vec<T>::pack(&g[j * P]) : zero;
+            for (int h = 0; h < kQ; ++h) {
+                if (p.want & 4) accumulate(place(2) + (j * kQ + h) * threads, &pre1[j * P + 2 * h], false);
+                if (p.want & 8) accumulate(place(3) + (j * kQ + h) * threads, &pre0[j * P + 2 * h], false);
             }
+        // the block's workers together, in their order
+        __syncthreads();
+        for (int i = threadIdx.x; i < wanted * per_sum; i += blockDim.x) {
+            const int which = i / per_sum, rest = i - which * per_sum;   // (sum, (vector, quarter), thread)
+            int k = p.want;                                              // the which-th bit that is set
+            for (int b = 0; b < which; ++b) k &= k - 1;
+            k = __ffs(k) - 1;
+            if (k == 4 && !p.one_gate) continue;
+            const int jh = rest / threads, v = rest % threads + jh / kQ * threads;
+            if (v >= p.vecs) continue;
+            float4 s = sums_s[i];
+            for (int w = 1; w < p.per_block; ++w) {
+                const float4 q = sums_s[(int64_t)w * wanted * per_sum + i];
+                s = make_float4(s.x + q.x, s.y + q.y, s.z + q.z, s.w + q.w);
+            }
+            reinterpret_cast<float4*>(p.sums + ((int64_t)k * p.blocks + blockIdx.x) * C + (int64_t)v * VN)[jh % kQ] = s;
         }
-        if constexpr (kSplit) __syncwarp();
-    }
-    if (gate_rows && lo < hi) put_gate();
-    // the block's workers together, in their order
-    __syncthreads();
-    for (int i = threadIdx.x; i < wanted * per_sum; i += blockDim.x) {
-        const int which = i / per_sum, rest = i - which * per_sum;   // (sum, (vector, quarter), thread)
-        int k = p.want;                                              // the which-th bit that is set
-        for (int b = 0; b < which; ++b) k &= k - 1;
-        k = __ffs(k) - 1;
-        if (k == 4 && !p.one_gate) continue;
-        const int jh = rest / threads, v = rest % threads + jh / kQ * threads;
-        if (v >= p.vecs) continue;
-        float4 s = sums_s[i];
-        for (int w = 1; w < p.per_block; ++w) {
-            const float4 q = sums_s[(int64_t)w * wanted * per_sum + i];
-            s = make_float4(s.x + q.x, s.y + q.y, s.z + q.z, s.w + q.w);
+        if (p.dY != nullptr) {                            // rows past M_keep are cleared
+            const int64_t warps = (int64_t)p.blocks * (blockDim.x >> 5), me = (int64_t)blockIdx.x * (blockDim.x >> 5) + warp;
+            for (int64_t m = M_keep + me; m < p.M_keep_cap; m += warps)
+                for (int v = lane; v < p.vecs; v += 32) p.dY[m * p.vecs + v] = zero;
         }
-        reinterpret_cast<float4*>(p.sums + ((int64_t)k * gridDim.x + blockIdx.x) * C + (int64_t)v * VN)[jh % kQ] = s;
     }
-    const int64_t warps = (int64_t)gridDim.x * (blockDim.x >> 5), me = (int64_t)blockIdx.x * (blockDim.x >> 5) + warp;
-    if (p.dY != nullptr) {                            // rows past M_keep are cleared
-        for (int64_t m = M_keep + me; m < p.M_keep_cap; m += warps)
-            for (int v = lane; v < p.vecs; v += 32) p.dY[m * p.vecs + v] = zero;
-    }
-    // the rows outside the list take the residual's gradient alone; every warp has its share of all rows
-    if (p.copy_rest) {
+    // the rows outside the list take the residual's gradient alone; every warp - of the blocks that do nothing else, if there are
+    // any - has its share of all rows
+    const int copy_from = (int)gridDim.x > p.blocks ? p.blocks : 0;
+    const int64_t warps = ((int64_t)gridDim.x - copy_from) * (blockDim.x >> 5), me = ((int64_t)blockIdx.x - copy_from) * (blockDim.x >> 5) + warp;
+    if (p.copy_rest && me >= 0) {
         const int64_t from = p.M * me / warps, to = p.M * (me + 1) / warps;
         warp_visit_dropped_rows(p.keep_rows, M_keep, from, to, lane, [&](int64_t base, uint32_t todo) {
-            // four rows at a time, 32 vectors of each: their loads before their stores
-            constexpr int kB = 4;
+            // eight rows at a time, 32 vectors of each: their loads before their stores
+            constexpr int kB = 8;
             while (todo) {
                 int64_t at[kB];
 #pragma unroll
@@ -600,7 +654,8 @@ __global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormR
                 b = r1 < M_keep ? r1 : M_keep;
             } else {
                 a = warp_lower_bound(p.keep_rows, M_keep, r0, lane);
-                b = warp_lower_bound(p.keep_rows, M_keep, r1, lane);
+                const int64_t most = a + p.gate_group < M_keep ? p.gate_group : M_keep - a;
+                b = a + warp_lower_bound(p.keep_rows + a, most, r1, lane);
             }
             const int64_t w0 = a < b ? a / chunk : 0, w1 = a < b ? (b - 1) / chunk + 1 : 0;
             // inside one worker's rows it is already written
@@ -633,29 +688,30 @@ inline FastDiv group_div(const void* gate, int64_t gate_group, int64_t M) { retu
 struct NormShape {
     int vecs, nv, lanes, warps, per;                  // vectors of a row, of a thread; lanes of a row (0: warps of it); numbers of a vector
 };
-// Eight numbers a thread up to 1024 channels: several rows a warp up to 128 channels, several warps a row from 256 on.  (Rows of up to
-// 1024 channels in one warp, up to 32 numbers a thread, take fewer instructions but leave registers for 14 warps an SM, which
-// spend ten cycles an instruction: 25088 x 768 forward 52 us.)  Beyond, 16 or 32 numbers.
+// Eight numbers a thread up to 1024 channels (backward: 4096): several rows a warp up to 128 channels, several warps a row from 256
+// on.  (Rows of up to 1024 channels in one warp, up to 32 numbers a thread, take fewer instructions but leave registers for 14
+// warps an SM, which spend ten cycles an instruction: 25088 x 768 forward 52 us.)  Beyond, 16 or 32 numbers.
 inline NormShape norm_shape(sbp_dtype dt, int64_t C, bool backward) {
     NormShape s;
     s.per = dt == SBP_BF16 ? 8 : 4;
     s.vecs = (int)(C / s.per);
     s.lanes = C <= 64 ? 8 : C <= 128 ? 16 : C <= 256 ? 32 : 0;
-    s.nv = C <= 1024 ? 8 / s.per : backward && dt == SBP_BF16 ? 2 : 4;
+    s.nv = C <= (backward ? 4096 : 1024) ? 8 / s.per : backward && dt == SBP_BF16 ? 2 : 4;
     s.warps = s.lanes > 0 ? 1 : (s.vecs + 32 * s.nv - 1) / (32 * s.nv);
     return s;
 }
+inline bool norm_many_warps(const NormShape& s) { return s.warps > 4; }
 // Backward blocks: as many workers as the sums of one leave room for in shared memory, up to 16 warps
 constexpr size_t kNormSmem = 200 * 1024;
 static_assert(kNormSmem >= (size_t)kNormSums * kNormMaxC * 4, "the sums of one worker");
 inline int norm_per_block(const NormShape& s, int sums) {
     const int threads = s.lanes > 0 ? s.lanes : 32 * s.warps;
-    const size_t bytes = (size_t)(sums > 0 ? sums : 1) * threads * s.nv * s.per * 4;
+    const size_t bytes = (size_t)threads * (sums > 0 ? sums : 1) * s.nv * s.per * 4;
     int64_t n = (int64_t)(kNormSmem / bytes);
-    const int most = norm_backward_threads(s.nv * s.per) / threads;
+    const int most = norm_backward_threads(s.nv * s.per, norm_many_warps(s)) / threads;
     if (n > most) n = most;
     if (s.lanes > 0) n = n / (32 / s.lanes) * (32 / s.lanes);        // whole warps
-    else if (n > kNormMostWorkers) n = kNormMostWorkers;
+    else if (n > (norm_many_warps(s) ? 1 : kNormMostWorkers)) n = norm_many_warps(s) ? 1 : kNormMostWorkers;
     return n < 1 ? 1 : (int)n;
 }
 
@@ -663,7 +719,7 @@ struct NormGrid {
     int blocks, per_block;
     int64_t workers;
 };
-// a block an SM; few rows: as many workers as rows (or as a quarter of the rows outside the list), over the blocks evenly
+// a block an SM; few rows: as many workers as rows (or as a quarter of the rows outside the list, which they copy), over the blocks evenly
 inline NormGrid norm_grid(const NormShape& s, int sums, int64_t M, int64_t M_keep_cap) {
     NormGrid g;
     if ((M - M_keep_cap + 3) / 4 > M_keep_cap) M_keep_cap = (M - M_keep_cap + 3) / 4;
@@ -677,13 +733,13 @@ inline NormGrid norm_grid(const NormShape& s, int sums, int64_t M, int64_t M_kee
     return g;
 }
 
-template <typename T, int kNV, int kLanes, bool kFull, typename Params>
+template <typename T, int kNV, int kLanes, bool kMany, bool kFull, typename Params>
 cudaError_t launch_norm(const Params& p, bool layer, bool post, dim3 grid, dim3 block, size_t smem, cudaStream_t stream) {
     auto with = [&](auto layer_c, auto post_c) {
         if constexpr (std::is_same_v<Params, NormFwdParams>) {
             return launch_pdl(norm_forward_kernel<T, kNV, kLanes, kFull, decltype(layer_c)::value, decltype(post_c)::value>, grid, block, smem, stream, p);
         } else {
-            constexpr auto kernel = norm_backward_kernel<T, kNV, kLanes, kFull, decltype(layer_c)::value, decltype(post_c)::value>;
+            constexpr auto kernel = norm_backward_kernel<T, kNV, kLanes, kMany, kFull, decltype(layer_c)::value, decltype(post_c)::value>;
             const cudaError_t e = opt_in_dynamic_smem<kernel>((int)kNormSmem);
             return e == cudaSuccess ? launch_pdl(kernel, grid, block, smem, stream, p) : e;
         }
@@ -696,18 +752,23 @@ template <typename T, typename Params>
 cudaError_t pick_norm(const NormShape& s, const Params& p, bool layer, bool post, dim3 grid, dim3 block, size_t smem, cudaStream_t stream) {
     constexpr bool kBackward = std::is_same_v<Params, NormBwdParams>, kWide = std::is_same_v<T, float>;
     const bool full = s.vecs == s.nv * (s.lanes > 0 ? s.lanes : 32 * s.warps);
-    auto with = [&](auto nv, auto lanes) {
-        return full ? launch_norm<T, decltype(nv)::value, decltype(lanes)::value, true>(p, layer, post, grid, block, smem, stream)
-                    : launch_norm<T, decltype(nv)::value, decltype(lanes)::value, false>(p, layer, post, grid, block, smem, stream);
+    auto with = [&](auto nv, auto lanes, auto many) {
+        return full ? launch_norm<T, decltype(nv)::value, decltype(lanes)::value, decltype(many)::value, true>(p, layer, post, grid, block, smem, stream)
+                    : launch_norm<T, decltype(nv)::value, decltype(lanes)::value, decltype(many)::value, false>(p, layer, post, grid, block, smem, stream);
     };
     constexpr std::integral_constant<int, kWide ? 2 : 1> eight;      // vectors of eight numbers
-    if (s.lanes == 8) return with(eight, std::integral_constant<int, 8>());
-    if (s.lanes == 16) return with(eight, std::integral_constant<int, 16>());
-    if (s.lanes == 32) return with(eight, std::integral_constant<int, 32>());
+    const std::false_type few;
+    if (s.lanes == 8) return with(eight, std::integral_constant<int, 8>(), few);
+    if (s.lanes == 16) return with(eight, std::integral_constant<int, 16>(), few);
+    if (s.lanes == 32) return with(eight, std::integral_constant<int, 32>(), few);
     const std::integral_constant<int, 0> warps;
-    if (s.nv == eight) return with(eight, warps);
-    if constexpr (kBackward && !kWide) return with(std::integral_constant<int, 2>(), warps);
-    else return with(std::integral_constant<int, 4>(), warps);
+    if constexpr (kBackward) {
+        const std::true_type many;
+        if (s.nv == eight) return norm_many_warps(s) ? with(eight, warps, many) : with(eight, warps, few);
+        return with(std::integral_constant<int, kWide ? 4 : 2>(), warps, many);
+    } else {
+        return s.nv == eight ? with(eight, warps, few) : with(std::integral_constant<int, 4>(), warps, few);
+    }
 }
 
 }  // namespace
@@ -800,6 +861,7 @@ cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR,
     const NormGrid g = norm_grid(s, sums, M, M_keep_cap);
     p.per_block = g.per_block;
     p.workers = g.workers;
+    p.blocks = g.blocks;
     p.sums = workspace;
     p.gate_sums = workspace + (size_t)kNormSums * g.blocks * C;
     p.vecs = s.vecs;
@@ -810,8 +872,10 @@ cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR,
     p.eps = eps;
     p.inv_c = 1.f / (float)C;
     const int threads = s.lanes > 0 ? s.lanes : 32 * s.warps;
-    const size_t smem = (size_t)sums * g.per_block * threads * s.nv * s.per * 4;
-    const dim3 grid((unsigned)g.blocks), block((unsigned)(g.per_block * threads));
+    const size_t smem = (size_t)g.per_block * threads * sums * s.nv * s.per * 4;
+    // few rows leave SMs free: blocks there copy the rows outside the list meanwhile
+    const int64_t idle = p.copy_rest && M > M_keep_cap && g.blocks < kNumSMs ? kNumSMs - g.blocks : 0, wanted_copies = (M + 3) / 4;
+    const dim3 grid((unsigned)(g.blocks + (idle < wanted_copies ? idle : wanted_copies))), block((unsigned)(g.per_block * threads));
     const bool post = post_w != nullptr;
     const cudaError_t e = dt == SBP_BF16 ? pick_norm<__nv_bfloat16>(s, p, layer, post, grid, block, smem, stream)
                                          : pick_norm<float>(s, p, layer, post, grid, block, smem, stream);

@@ -75,18 +75,19 @@ __device__ __forceinline__ void load_f32(const float* p, f32x2* f) {
 }
 
 // The threads that share a row: kLanes (8, 16 or 32) of a warp, or, kLanes 0, `warps` warps of a block, which meet at barrier `id`
-// and add up through `scratch`: two halves of a float4 a warp, taken in turns - a half is written again only after the barrier of
+// and add up through `scratch`: two halves of 32 float4, taken in turns - a half is written again only after the barrier of
 // the sum between, by which every thread has read it.
 template <int kLanes>
 struct RowThreads {
     static constexpr bool kMulti = kLanes == 0;
+    static constexpr int kHalf = 32;                  // float4 of half of `scratch`: 16 warps of eight values
     int t, count;                                     // this thread, of how many
     int warps, id, turn;
     float4* scratch;
     __device__ __forceinline__ int threads() const { return kMulti ? count : kLanes; }
 
-    // Sums of V <= 4 values over those threads, in an order that depends on their number alone.  Several values over 32 lanes take
-    // six exchanges: each of the first two halves what a lane carries.
+    // Sums of V <= 8 values over those threads, in an order that depends on their number alone.  Several values over 32 lanes: the first
+    // exchanges halve what a lane carries, so that 4 or 8 values take 6 or 9 of them.
     template <int V>
     __device__ __forceinline__ void sums(float (&v)[V]) {
         const int lane = threadIdx.x & 31;
@@ -97,43 +98,53 @@ struct RowThreads {
                 for (int i = 0; i < V; ++i) v[i] += __shfl_xor_sync(0xffffffffu, v[i], o);
             if constexpr (!kMulti) return;
         }
+        constexpr int kSlots = V > 4 ? 8 : 4, kEach = 32 / kSlots;   // lanes kEach i .. come to hold the sum of value i
         float s = v[0];
-        if constexpr (V > 1) {                        // lanes 8 k .. 8 k + 7 come to hold the sum of value k
-            const bool h4 = lane & 16, h3 = lane & 8;
-            const float v2 = V > 2 ? v[V > 2 ? 2 : 0] : 0.f, v3 = V > 3 ? v[V > 3 ? 3 : 0] : 0.f;
-            float a = h4 ? v2 : v[0], b = h4 ? v3 : v[1];
-            a += __shfl_xor_sync(0xffffffffu, h4 ? v[0] : v2, 16);
-            b += __shfl_xor_sync(0xffffffffu, h4 ? v[1] : v3, 16);
-            s = h3 ? b : a;
-            s += __shfl_xor_sync(0xffffffffu, h3 ? a : b, 8);
-            s += __shfl_xor_sync(0xffffffffu, s, 4);
-            s += __shfl_xor_sync(0xffffffffu, s, 2);
-            s += __shfl_xor_sync(0xffffffffu, s, 1);
+        if constexpr (V > 1) {
+            float f[kSlots];
+#pragma unroll
+            for (int i = 0; i < kSlots; ++i) f[i] = i < V ? v[i < V ? i : 0] : 0.f;
+#pragma unroll
+            for (int n = kSlots / 2, o = 16; n > 0; n /= 2, o /= 2) {
+                const bool upper = lane & o;
+#pragma unroll
+                for (int i = 0; i < n; ++i) {
+                    const float send = upper ? f[i] : f[i + n], keep = upper ? f[i + n] : f[i];
+                    f[i] = keep + __shfl_xor_sync(0xffffffffu, send, o);
+                }
+            }
+            s = f[0];
+#pragma unroll
+            for (int o = kEach / 2; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
         }
         if constexpr (!kMulti) {
 #pragma unroll
-            for (int i = 0; i < V; ++i) v[i] = __shfl_sync(0xffffffffu, s, 8 * i);
+            for (int i = 0; i < V; ++i) v[i] = __shfl_sync(0xffffffffu, s, kEach * i);
         } else {
-            float4* half = scratch + (turn ? 16 : 0);
+            constexpr int kQuads = kSlots / 4;
+            float4* half = scratch + (turn ? kHalf : 0);
             turn ^= 1;
-            if ((lane & 7) == 0) reinterpret_cast<float*>(half + (t >> 5))[lane >> 3] = s;     // (V == 1: the sum four times)
+            if (lane % kEach == 0) reinterpret_cast<float*>(half + (t >> 5) * kQuads)[lane / kEach] = s;       // (V == 1: the sum four times)
             asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(count) : "memory");
-            float4 f = half[0];
+            float4 f[kQuads];
+#pragma unroll
+            for (int i = 0; i < kQuads; ++i) f[i] = half[i];
             auto more = [&](int w) {
-                const float4 q = half[w];
-                f.x += q.x;
-                if constexpr (V > 1) f.y += q.y;
-                if constexpr (V > 2) f.z += q.z;
-                if constexpr (V > 3) f.w += q.w;
+#pragma unroll
+                for (int i = 0; i < kQuads; ++i) {
+                    const float4 q = half[w * kQuads + i];
+                    f[i].x += q.x;
+                    f[i].y += q.y;
+                    f[i].z += q.z;
+                    f[i].w += q.w;
+                }
             };
             if (warps > 1) more(1);
             if (warps > 2) more(2);
             if (warps > 3) more(3);
             for (int w = 4; w < warps; ++w) more(w);
-            v[0] = f.x;
-            if constexpr (V > 1) v[1] = f.y;
-            if constexpr (V > 2) v[2] = f.z;
-            if constexpr (V > 3) v[3] = f.w;
+#pragma unroll
+            for (int i = 0; i < V; ++i) v[i] = i % 4 == 0 ? f[i / 4].x : i % 4 == 1 ? f[i / 4].y : i % 4 == 2 ? f[i / 4].z : f[i / 4].w;
         }
     }
 };
