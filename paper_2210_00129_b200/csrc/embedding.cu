@@ -8,11 +8,14 @@
 // cross a piece's border leaves partial rows, which a last launch adds in the order of the pieces.  Nothing depends on how
 // often an id occurs: the most frequent one is spread over as many pieces as its rows fill.
 //
-// Bound by memory, in the main by clearing dTable where few of its rows get a gradient (50257 x 768: 154 MB).  The sort of
-// some ten thousand ids is a handful of short launches that leave the memory idle, so that blocks of those launches clear the
-// table, and the sums then write over the rows that have one.
+// Bound by memory, in the main by clearing dTable where few of its rows get a gradient (50257 x 768: 154 MB), and for small tables by
+// latency.  Up to 131072 rows are sorted by one cluster of blocks in one launch, which exchange their digits' counts through
+// distributed shared memory; the other blocks of that launch clear the table meanwhile, and the sums then write over the rows
+// that have one.  (Four to six launches of separate counts and scatters: 31 us for 12544 rows and one digit.)  Longer lists take
+// two launches a digit.
 #include "row_copy.cuh"
 #include "row_math.cuh"
+#include "tc_ptx.cuh"
 
 namespace sbp {
 namespace {
@@ -64,6 +67,8 @@ embedding_forward_kernel(const uint4* __restrict__ table, const RowLength row, i
 // ---- backward: the sort ----
 constexpr int kSortThreads = 512, kSortItems = 8, kSortTile = kSortThreads * kSortItems, kSortWarps = kSortThreads / 32;
 constexpr int kDigits = 256, kSortMaxBlocks = 128;
+constexpr int kSortCluster = 8;
+constexpr int64_t kSortClusterRows = 131072;          // four tiles a block of the cluster
 
 struct SortParams {
     const int32_t *ids, *keep_rows, *M_keep_dev;
@@ -72,22 +77,12 @@ struct SortParams {
     uint32_t* keys[2];
     int32_t* rows[2];
     uint32_t* hist;                                   // [blocks][kDigits]
-    int tiles;                                        // kSortTile pieces of a block
+    int64_t span;                                     // rows of a block
     int blocks, passes, bits;                         // sorting blocks; digits of `bits` bits
     uint4* clear;                                     // dTable, or nullptr
     int64_t clear_vecs;
     int32_t* status_word;
 };
-
-// The id of the m-th kept row (V: none), and where its gradient is.
-__device__ __forceinline__ uint32_t sort_input(const SortParams& p, int64_t m, int32_t* src) {
-    const int64_t row = mapped_row(p.keep_rows, m);
-    *src = p.compact ? (int32_t)m : (int32_t)row;
-    if (row < 0 || row >= p.M) return (uint32_t)p.V;
-    const int64_t id = __ldg(p.ids + row);
-    if (id >= p.V) report_device_error(p.status_word, SBP_ERR_BAD_INDICES);
-    return id >= 0 && id < p.V ? (uint32_t)id : (uint32_t)p.V;
-}
 
 // Blocks behind the sorting ones clear `part` of `parts` of dTable.
 __device__ __forceinline__ void clear_table(const SortParams& p, int part, int parts) {
@@ -115,7 +110,8 @@ __device__ __forceinline__ uint32_t digit_scan(uint32_t v, uint32_t* warp_sums) 
     if (lane == 31 && warp < kDigits / 32) warp_sums[warp] = s;
     __syncthreads();
     uint32_t before = 0;
-    for (int w = 0; w < warp && w < kDigits / 32; ++w) before += warp_sums[w];
+#pragma unroll
+    for (int w = 0; w < kDigits / 32; ++w) before += w < warp ? warp_sums[w] : 0u;
     __syncthreads();
     return before + s - v;
 }
@@ -126,12 +122,54 @@ struct SortShared {
     uint32_t warp_sums[kDigits / 32];
 };
 
+// Counts of the digits of elements [begin, end), left in sh.base.  The first pass makes the keys: the id of the m-th kept row (V:
+// none), and where its gradient is; a tile's loads are under way together.
+__device__ __forceinline__ void count_digits(const SortParams& p, SortShared& sh, int64_t begin, int64_t end, int pass) {
+    if (threadIdx.x < kDigits) sh.base[threadIdx.x] = 0u;
+    __syncthreads();
+    const uint32_t mask = (1u << p.bits) - 1u;
+    for (int64_t tile = begin; tile < end; tile += kSortTile) {
+        uint32_t key[kSortItems];
+        if (pass == 0) {
+            int32_t row[kSortItems], id[kSortItems];
+#pragma unroll
+            for (int i = 0; i < kSortItems; ++i) {
+                const int64_t at = tile + threadIdx.x + i * kSortThreads;
+                row[i] = at < end ? mapped_row(p.keep_rows, at) : -1;
+            }
+            bool bad = false;
+#pragma unroll
+            for (int i = 0; i < kSortItems; ++i) id[i] = __ldg(p.ids + (row[i] >= 0 && row[i] < p.M ? row[i] : 0));
+#pragma unroll
+            for (int i = 0; i < kSortItems; ++i) {
+                const int64_t at = tile + threadIdx.x + i * kSortThreads;
+                const bool ok = row[i] >= 0 && row[i] < p.M;
+                bad |= ok && id[i] >= p.V;
+                key[i] = ok && id[i] >= 0 && id[i] < p.V ? (uint32_t)id[i] : (uint32_t)p.V;
+                if (at < end) {
+                    p.keys[1][at] = key[i];
+                    p.rows[1][at] = p.compact ? (int32_t)at : row[i];
+                }
+            }
+            if (bad) report_device_error(p.status_word, SBP_ERR_BAD_INDICES);
+        } else {
+#pragma unroll
+            for (int i = 0; i < kSortItems; ++i) {
+                const int64_t at = tile + threadIdx.x + i * kSortThreads;
+                key[i] = at < end ? __ldcg(p.keys[(pass + 1) & 1] + at) : 0u;
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < kSortItems; ++i)
+            if (tile + threadIdx.x + i * kSortThreads < end) atomicAdd(&sh.base[key[i] >> (pass * p.bits) & mask], 1u);
+    }
+    __syncthreads();
+}
+
 // Elements [begin, begin + kSortTile) of the list, below n: each goes to base[digit] plus the number of elements of its digit
 // before it; base moves on.  Warp w has the w-th 256 elements, 32 at a time, so the order of the list is kept.
 __device__ __forceinline__ void scatter_tile(const SortParams& p, SortShared& sh, int64_t begin, int64_t n, int pass) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&sh.count[0][0])[i] = 0u;
-    __syncthreads();
     uint32_t key[kSortItems], rank[kSortItems];
     int32_t row[kSortItems];
     const int shift = pass * p.bits;
@@ -140,22 +178,18 @@ __device__ __forceinline__ void scatter_tile(const SortParams& p, SortShared& sh
 #pragma unroll
     for (int i = 0; i < kSortItems; ++i) {
         const int64_t at = first + 32 * i;
-        key[i] = 0u;
-        row[i] = 0;
-        if (at < n) {
-            if (pass == 0) key[i] = sort_input(p, at, &row[i]);
-            else {
-                key[i] = p.keys[(pass + 1) & 1][at];
-                row[i] = p.rows[(pass + 1) & 1][at];
-            }
-        }
+        key[i] = at < n ? __ldcg(p.keys[(pass + 1) & 1] + at) : 0u;
+        row[i] = at < n ? __ldcg(p.rows[(pass + 1) & 1] + at) : 0;
     }
+    for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&sh.count[0][0])[i] = 0u;
+    __syncthreads();
 #pragma unroll
     for (int i = 0; i < kSortItems; ++i) {
         const bool live = first + 32 * i < n;
         const uint32_t d = key[i] >> shift & mask;
         uint32_t peers = __ballot_sync(0xffffffffu, live);
-        for (int b = 0; b < p.bits; ++b) {
+#pragma unroll
+        for (int b = 0; b < 8; ++b) {
             const uint32_t set = __ballot_sync(0xffffffffu, d >> b & 1u);
             peers &= (d >> b & 1u) ? set : ~set;
         }
@@ -168,6 +202,7 @@ __device__ __forceinline__ void scatter_tile(const SortParams& p, SortShared& sh
     __syncthreads();
     if (threadIdx.x < kDigits) {                      // a warp's elements of a digit follow those of the warps before it
         uint32_t at = sh.base[threadIdx.x];
+#pragma unroll
         for (int w = 0; w < kSortWarps; ++w) {
             const uint32_t c = sh.count[w][threadIdx.x];
             sh.count[w][threadIdx.x] = at;
@@ -186,32 +221,38 @@ __device__ __forceinline__ void scatter_tile(const SortParams& p, SortShared& sh
     __syncthreads();
 }
 
-// Counts of the digits of elements [begin, end), left in sh.base.
-__device__ __forceinline__ void count_digits(const SortParams& p, SortShared& sh, int64_t begin, int64_t end, int pass) {
-    if (threadIdx.x < kDigits) sh.base[threadIdx.x] = 0u;
-    __syncthreads();
-    const uint32_t mask = (1u << p.bits) - 1u;
-    for (int64_t at = begin + threadIdx.x; at < end; at += kSortThreads) {
-        int32_t src;
-        const uint32_t key = pass == 0 ? sort_input(p, at, &src) : p.keys[(pass + 1) & 1][at];
-        atomicAdd(&sh.base[key >> (pass * p.bits) & mask], 1u);
-    }
-    __syncthreads();
-}
-
-// The whole sort in one block.
+// The whole sort by the first cluster, which the others' clearing hides.
 __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(const SortParams p) {
     __shared__ SortShared sh;
+    __shared__ uint32_t counts[kSortCluster][kDigits];               // of every block of the cluster
     pdl_launch_dependents();
     pdl_wait();
     if (blockIdx.x >= (unsigned)p.blocks) return clear_table(p, 0, 1);
     const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap);
+    const uint32_t rank = ptx::cluster_ctarank();
+    const int64_t begin = rank * p.span < n ? rank * p.span : n, end = begin + p.span < n ? begin + p.span : n;
+    ptx::cluster_sync_all();                                         // every block has begun
     for (int pass = 0; pass < p.passes; ++pass) {
-        count_digits(p, sh, 0, n, pass);
-        const uint32_t start = digit_scan(threadIdx.x < kDigits ? sh.base[threadIdx.x] : 0u, sh.warp_sums);
-        if (threadIdx.x < kDigits) sh.base[threadIdx.x] = start;
+        count_digits(p, sh, begin, end, pass);
+        if (threadIdx.x < kDigits)
+            for (uint32_t b = 0; b < kSortCluster; ++b)
+                asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(ptx::map_to_cta(ptx::smem_addr(&counts[rank][threadIdx.x]), b)),
+                             "r"(sh.base[threadIdx.x]) : "memory");
+        ptx::cluster_sync_all();
+        uint32_t all = 0u, before = 0u;
+        if (threadIdx.x < kDigits) {
+#pragma unroll
+            for (uint32_t b = 0; b < kSortCluster; ++b) {
+                const uint32_t c = counts[b][threadIdx.x];
+                all += c;
+                before += b < rank ? c : 0u;
+            }
+        }
+        const uint32_t start = digit_scan(all, sh.warp_sums);
+        if (threadIdx.x < kDigits) sh.base[threadIdx.x] = start + before;
         __syncthreads();
-        scatter_tile(p, sh, 0, n, pass);
+        for (int64_t at = begin; at < end; at += kSortTile) scatter_tile(p, sh, at, end, pass);
+        ptx::cluster_sync_all();                                     // the list is in its new order, and all have read the counts
     }
 }
 
@@ -221,8 +262,8 @@ __global__ void __launch_bounds__(kSortThreads) embedding_count_kernel(const Sor
     pdl_launch_dependents();
     pdl_wait();
     if (blockIdx.x >= (unsigned)p.blocks) return clear_table(p, 2 * pass, 2 * p.passes);
-    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap), span = (int64_t)p.tiles * kSortTile;
-    const int64_t begin = blockIdx.x * span, end = begin + span < n ? begin + span : n;
+    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap);
+    const int64_t begin = blockIdx.x * p.span, end = begin + p.span < n ? begin + p.span : n;
     count_digits(p, sh, begin, end, pass);
     if (threadIdx.x < kDigits) p.hist[blockIdx.x * kDigits + threadIdx.x] = sh.base[threadIdx.x];
 }
@@ -231,8 +272,8 @@ __global__ void __launch_bounds__(kSortThreads) embedding_scatter_kernel(const S
     pdl_launch_dependents();
     pdl_wait();
     if (blockIdx.x >= (unsigned)p.blocks) return clear_table(p, 2 * pass + 1, 2 * p.passes);
-    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap), span = (int64_t)p.tiles * kSortTile;
-    const int64_t begin = blockIdx.x * span, end = begin + span < n ? begin + span : n;
+    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap);
+    const int64_t begin = blockIdx.x * p.span, end = begin + p.span < n ? begin + p.span : n;
     if (begin >= end) return;
     uint32_t all = 0u, before = 0u;
     if (threadIdx.x < kDigits) {
@@ -246,7 +287,7 @@ __global__ void __launch_bounds__(kSortThreads) embedding_scatter_kernel(const S
     const uint32_t start = digit_scan(all, sh.warp_sums);
     if (threadIdx.x < kDigits) sh.base[threadIdx.x] = start + before;
     __syncthreads();
-    for (int64_t at = begin; at < end; at += kSortTile) scatter_tile(p, sh, at, n, pass);
+    for (int64_t at = begin; at < end; at += kSortTile) scatter_tile(p, sh, at, end, pass);
 }
 
 // ---- backward: the sums ----
@@ -355,11 +396,15 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumParams p) 
     if (k >= (uint32_t)p.V || p.keys[hi] != k || (lo > 0 && p.keys[lo - 1] == k)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t pieces = (n + p.piece - 1) / p.piece;
-    int64_t end = piece + 2, top = pieces;            // pieces [piece + 1, end) begin with this id
+    // pieces [piece + 1, end) begin with this id (the list is sorted: 32 probes a step)
+    int64_t end = piece + 2, top = pieces;
     while (end < top) {
-        const int64_t mid = (end + top) / 2;
-        if (p.keys[mid * p.piece] == k) end = mid + 1;
-        else top = mid;
+        const int64_t step = (top - end + 31) / 32, at = end + lane * step;
+        const int same = __popc(__ballot_sync(0xffffffffu, at < top && p.keys[(at < top ? at : end) * p.piece] == k));
+        if (same == 0) break;
+        const int64_t last = end + (same - 1) * step;
+        end = last + 1;
+        top = last + step < top ? last + step : top;
     }
     const int v = (int)(blockIdx.x % p.strips) * 32 + lane;
     const int64_t C = (int64_t)p.vecs * N;
@@ -391,18 +436,19 @@ struct SumShape {
     int strips, piece;
     int64_t pieces;
 };
-// pieces: enough warps for the device (32 an SM), and eight places at least, so that a piece's own loads overlap
+// pieces: enough warps for the device (16 an SM: more leave more partial rows), and eight places at least, so that a piece's own loads overlap
 inline SumShape sum_shape(sbp_dtype dt, int64_t M_keep_cap, int64_t C) {
     SumShape s;
     const int64_t vecs = C / (dt == SBP_BF16 ? 8 : 4);
     s.strips = (int)((vecs + 31) / 32);
-    const int64_t want = (int64_t)kNumSMs * 32 / s.strips, p = (M_keep_cap + want) / (want > 0 ? want : 1);
+    const int64_t want = (int64_t)kNumSMs * 16 / s.strips, p = (M_keep_cap + want) / (want > 0 ? want : 1);
     s.piece = (int)(p < 8 ? 8 : p);
     s.pieces = (M_keep_cap + s.piece - 1) / s.piece;
     return s;
 }
 struct SortShape {
-    int blocks, tiles, passes, bits;
+    int blocks, passes, bits;
+    int64_t span;
 };
 inline SortShape sort_shape(int64_t M_keep_cap, int64_t V) {
     SortShape s;
@@ -410,10 +456,9 @@ inline SortShape sort_shape(int64_t M_keep_cap, int64_t V) {
     while ((V >> bits) != 0) ++bits;                  // keys 0 .. V
     s.passes = (bits + 7) / 8;
     s.bits = (bits + s.passes - 1) / s.passes;
-    const int64_t tiles = (M_keep_cap + kSortTile - 1) / kSortTile;
-    s.tiles = (int)((tiles + kSortMaxBlocks - 1) / kSortMaxBlocks);
-    if (s.tiles < 1) s.tiles = 1;
-    s.blocks = (int)((tiles + s.tiles - 1) / s.tiles);
+    const int64_t unit = M_keep_cap <= kSortClusterRows ? 32 : kSortTile, most = M_keep_cap <= kSortClusterRows ? kSortCluster : kSortMaxBlocks;
+    s.span = (M_keep_cap + unit * most - 1) / (unit * most) * unit;
+    s.blocks = M_keep_cap <= kSortClusterRows ? kSortCluster : (int)((M_keep_cap + s.span - 1) / s.span);
     return s;
 }
 inline size_t up256(size_t v) { return (v + 255) / 256 * 256; }
@@ -457,7 +502,7 @@ cudaError_t launch_embedding_backward(sbp_dtype dt, const void* dOut, bool compa
     p.rows[0] = (int32_t*)(ws + 2 * list);
     p.rows[1] = (int32_t*)(ws + 3 * list);
     p.hist = (uint32_t*)(ws + 4 * list);
-    p.tiles = so.tiles;
+    p.span = so.span;
     p.blocks = so.blocks;
     p.passes = so.passes;
     p.bits = so.bits;
@@ -465,13 +510,16 @@ cudaError_t launch_embedding_backward(sbp_dtype dt, const void* dOut, bool compa
     p.clear_vecs = V * (C / 4);
     p.status_word = status_word;
     const int64_t want = (p.clear_vecs + 4 * kSortThreads - 1) / (4 * kSortThreads);
-    const int clear_blocks = accumulate ? 0 : (int)(want < 2 * kNumSMs ? want : 2 * kNumSMs);
-    const dim3 grid((unsigned)(so.blocks + clear_blocks)), block(kSortThreads);
-    if (grid.x == 0) return cudaSuccess;              // no rows, and nothing to clear
+    int clear_blocks = accumulate ? 0 : (int)(want < 2 * kNumSMs ? want : 2 * kNumSMs);
+    const dim3 block(kSortThreads);
+    if (accumulate && M_keep_cap == 0) return cudaSuccess;           // nothing to add, and nothing to clear
     cudaError_t e;
-    if (so.blocks <= 1) {
-        if ((e = launch_pdl(embedding_sort_kernel, grid, block, 0, stream, p)) != cudaSuccess) return e;
+    if (M_keep_cap <= kSortClusterRows) {
+        clear_blocks = (clear_blocks + kSortCluster - 1) / kSortCluster * kSortCluster;
+        e = launch_pdl_cluster(embedding_sort_kernel, dim3((unsigned)(so.blocks + clear_blocks)), block, 0, kSortCluster, stream, p);
+        if (e != cudaSuccess) return e;
     } else {
+        const dim3 grid((unsigned)(so.blocks + clear_blocks));
         for (int pass = 0; pass < so.passes; ++pass) {
             if ((e = launch_pdl(embedding_count_kernel, grid, block, 0, stream, p, pass)) != cudaSuccess) return e;
             if ((e = launch_pdl(embedding_scatter_kernel, grid, block, 0, stream, p, pass)) != cudaSuccess) return e;
