@@ -18,7 +18,7 @@ def built():
     (dict(count=0), INV), (dict(rows=0), INV), (dict(cols=-1), INV), (dict(steps=0), INV), (dict(steps=33), INV), (dict(beta=float("nan")), INV),
     (dict(eps=-1e-9), INV), (dict(eps=float("inf")), INV), (dict(scale=1e300), INV), (dict(momentum=None, flags=sbp.SBP_FLAG_NESTEROV), INV),
     (dict(rows=2 ** 17), UNS), (dict(cols=2 ** 17), UNS), (dict(count=2 ** 16), UNS), (dict(workspace=None), WS), (dict(workspace=P + 16), WS),
-    (dict(workspace_bytes=1000), WS)])
+    (dict(workspace_bytes=255), WS), (dict(rows=640, cols=320, workspace_bytes=1000), WS)])
 def test_refusals(kw, status):
     a = dict(dt=1, G=P, momentum=P, beta=0.9, count=2, rows=64, cols=32, steps=5, eps=1e-7, scale=1.0, O=P, flags=0, workspace=P,
              workspace_bytes=1 << 30) | kw
