@@ -49,11 +49,11 @@ constexpr int kMostStages = 6, kItems = 4;
 
 enum { kGram = 0, kPoly = 1, kStep = 2 };
 
-struct OrthoControl {
+struct alignas(16) OrthoControl {
     uint64_t full[kMostStages], empty[kMostStages];                  // a stage's operands: in place, read
     uint64_t acc_full[2], acc_empty[2], small_full[2], small_empty[2];
     uint64_t item_full[kItems], item_empty[kItems], stored[kItems];  // an item: drawn and ready, read by all, its tile written
-    uint32_t item[kItems];
+    int4 item[kItems][2];            // its eight numbers
     uint32_t tmem_slot;
     int abort_flag;
 };
@@ -64,12 +64,15 @@ struct OrthoParams {
     float *diag_a, *diag_b;          // [count][ldm]
     void* out;                       // the last step's result [count][rows][cols]
     uint32_t* drawn;                 // items drawn so far
-    int32_t* done;                   // [count]: finished tiles of the matrix
+    int32_t* done;                   // [count]: finished items of the matrix
+    int32_t* shares;                 // [count][sym_tiles]: finished shares of A's tile that another item adds up
+    float4* share;                   // [cuts - 1][count][sym_tiles][128 x 128 sums]
     int64_t x_plane, s_plane;        // elements of one matrix's plane
     int count, rows, cols, m, ldx, ldm, steps;
     int b_plane;                     // of B's first numbers: 1, or 2 where A has second ones
     uint32_t sym_tiles, step_tiles, step_cols;       // of a matrix: tiles of A or B, of X; columns of tiles of X
     int gram_blocks, m_blocks;       // 64 deep blocks of A's reduction, and of the others
+    int cuts;                        // shares of A's reduction, where its tiles alone leave blocks idle
     int tall, out_bf16;
     float scale;
     int32_t* status_word;
@@ -78,20 +81,32 @@ struct OrthoParams {
 // a product's tile: rows 128 i and columns kWidth j of matrix `matrix`'s A, B or next X
 struct OrthoItem {
     int step, mode, matrix, i, j;
-    int32_t need;                    // of done[matrix]
+    int tile, cut;                   // A: which of the matrix's tiles, which share of its reduction
+    int32_t need;                    // of done[matrix]; -1: there are no more items
 };
 template <int kWidth>
 __device__ __forceinline__ OrthoItem ortho_item(const OrthoParams& p, uint32_t q) {
     OrthoItem t;
-    const uint32_t sym = p.sym_tiles * (uint32_t)p.count, per_step = 2 * sym + p.step_tiles * (uint32_t)p.count;
-    t.step = (int)(q / per_step);
-    uint32_t r = q - (uint32_t)t.step * per_step;
-    const uint32_t matrix_tiles = 2 * p.sym_tiles + p.step_tiles;
-    if (r < 2 * sym) {
-        t.mode = r < sym ? kGram : kPoly;
-        if (t.mode == kPoly) r -= sym;
-        t.matrix = (int)(r / p.sym_tiles);
-        r -= (uint32_t)t.matrix * p.sym_tiles;
+    const uint32_t gram_items = p.sym_tiles * (uint32_t)p.cuts, matrix_items = gram_items + p.sym_tiles + p.step_tiles;
+    t.step = (int)(q / (matrix_items * (uint32_t)p.count));
+    uint32_t r = q - (uint32_t)t.step * matrix_items * (uint32_t)p.count;
+    t.need = (int)((uint32_t)t.step * matrix_items);
+    t.cut = 0;
+    const uint32_t grams = gram_items * (uint32_t)p.count, polys = p.sym_tiles * (uint32_t)p.count;
+    if (r < grams + polys) {
+        t.mode = r < grams ? kGram : kPoly;
+        if (t.mode == kGram) {                                       // the shares of a tile one after the other: the last adds up
+            t.matrix = (int)(r / gram_items);
+            r -= (uint32_t)t.matrix * gram_items;
+            t.cut = (int)(r % (uint32_t)p.cuts);
+            r /= (uint32_t)p.cuts;
+        } else {
+            r -= grams;
+            t.matrix = (int)(r / p.sym_tiles);
+            r -= (uint32_t)t.matrix * p.sym_tiles;
+            t.need += (int)gram_items;
+        }
+        t.tile = (int)r;
         // column j has the tiles that reach the diagonal or lie above it: 128 j .. wide tiles j + 1 of them, 256 wide ones 2 j + 2
         constexpr uint32_t kF = kWidth / kTile;
         uint32_t j = (uint32_t)((sqrtf(8.f / kF * (float)r + 1.f) - 1.f) * 0.5f);
@@ -99,17 +114,22 @@ __device__ __forceinline__ OrthoItem ortho_item(const OrthoParams& p, uint32_t q
         while (kF * j * (j + 1) / 2 > r) --j;
         t.j = (int)j;
         t.i = (int)(r - kF * j * (j + 1) / 2);
-        t.need = (int)((uint32_t)t.step * matrix_tiles + (t.mode == kPoly ? p.sym_tiles : 0u));
     } else {
         t.mode = kStep;
-        r -= 2 * sym;
+        r -= grams + polys;
         t.matrix = (int)(r / p.step_tiles);
         r -= (uint32_t)t.matrix * p.step_tiles;
+        t.tile = (int)r;
         t.i = (int)(r / p.step_cols);
         t.j = (int)(r % p.step_cols);
-        t.need = (int)((uint32_t)t.step * matrix_tiles + 2 * p.sym_tiles);
+        t.need += (int)(gram_items + p.sym_tiles);
     }
     return t;
+}
+// the 64 deep blocks [from, from + n) of an item's reduction
+__device__ __forceinline__ int ortho_blocks(const OrthoParams& p, const OrthoItem& t, int& from) {
+    from = t.mode == kGram ? p.gram_blocks * t.cut / p.cuts : 0;
+    return t.mode == kGram ? p.gram_blocks * (t.cut + 1) / p.cuts - from : p.m_blocks;
 }
 
 // Waits (bounded, as every wait here) until `need` tiles of a matrix are finished; what they wrote is then visible to this
@@ -121,7 +141,7 @@ __device__ __forceinline__ bool wait_done(const int32_t* done, int32_t need, vol
         // (an acquiring load here, over and over, would empty the SM's L1 each time and hold up the other warps' loads)
         asm volatile("ld.relaxed.gpu.global.s32 %0, [%1];" : "=r"(v) : "l"(done) : "memory");
         if (v >= need) break;
-        __nanosleep(64);
+        __nanosleep(32);
         if (*abort_flag) return false;
         if (spins == 0) t0 = ptx::global_timer_ns();
         else if ((spins & 63u) == 0u && ptx::global_timer_ns() - t0 > ptx::kWaitLimitNs) {
@@ -251,6 +271,41 @@ __device__ __forceinline__ void give_back(OrthoWarp& w, uint64_t* empty, Turns& 
     ++t.used;
 }
 
+// Shares of a tile of A: a warp's sums, 32 columns of a row a lane, to where the warp of the same place in the last share's item finds
+// them; and those of all other shares added to that one's, in their order.
+__device__ __forceinline__ float4* share_place(const OrthoParams& p, const OrthoItem& t, const OrthoWarp& w, int cut, int col) {
+    const int64_t tile = ((int64_t)cut * p.count + t.matrix) * p.sym_tiles + t.tile;
+    return p.share + tile * (kTile * kTile / 4) + (w.quad * 4 + col / 32) * (32 * 8) + w.lane;       // (col: of the tile, a multiple of 32)
+}
+template <int kFrom, int kSize>
+__device__ __forceinline__ void put_share(const OrthoParams& p, const OrthoItem& t, const OrthoWarp& w, int col, const float (&v)[kSize]) {
+    float4* to = share_place(p, t, w, t.cut, col);
+#pragma unroll
+    for (int g = 0; g < 8; ++g) to[g * 32] = make_float4(v[kFrom + 4 * g], v[kFrom + 4 * g + 1], v[kFrom + 4 * g + 2], v[kFrom + 4 * g + 3]);
+}
+template <int kFrom, int kSize>
+__device__ __forceinline__ void add_shares(const OrthoParams& p, const OrthoItem& t, const OrthoWarp& w, int col, float (&v)[kSize]) {
+    for (int cut = 0; cut < p.cuts - 1; ++cut) {
+        const float4* from = share_place(p, t, w, cut, col);
+        float4 q[8];
+#pragma unroll
+        for (int g = 0; g < 8; ++g) q[g] = __ldcg(from + g * 32);
+#pragma unroll
+        for (int g = 0; g < 8; ++g) {
+            v[kFrom + 4 * g] += q[g].x;
+            v[kFrom + 4 * g + 1] += q[g].y;
+            v[kFrom + 4 * g + 2] += q[g].z;
+            v[kFrom + 4 * g + 3] += q[g].w;
+        }
+    }
+}
+__device__ __forceinline__ bool wait_shares(const OrthoParams& p, const OrthoItem& t, const OrthoWarp& w) {
+    bool ok = true;
+    if (w.lane == 0)
+        ok = wait_done(p.shares + (int64_t)t.matrix * p.sym_tiles + t.tile, (t.step + 1) * (p.cuts - 1), w.abort_flag, p.status_word);
+    return __all_sync(0xffffffffu, ok);
+}
+
 // The epilogue of one tile by one warp where the products take both numbers of every operand: 32 rows, 64 columns, 32 at a time.
 // The sums of the parts are added up in registers, then combined with numbers from memory.
 template <int kMode>
@@ -300,7 +355,8 @@ __device__ __forceinline__ bool ortho_epilogue_exact(const OrthoParams& p, const
 #pragma unroll
     for (int i = 0; i < kCols; ++i) sum[i] = 0.f;
     {
-        const int blocks = kMode == kGram ? p.gram_blocks : p.m_blocks;
+        int from_block;
+        const int blocks = ortho_blocks(p, t, from_block);
         auto add = [&](uint32_t taddr) {
 #pragma unroll
             for (int c = 0; c < kCols; c += 32) {
@@ -319,6 +375,18 @@ __device__ __forceinline__ bool ortho_epilogue_exact(const OrthoParams& p, const
         if (!take_sums(w, w.ctl->small_full, w.small, p.status_word)) return false;
         add(w.tmem + (2 + w.small.slot()) * kWidth + w.half * kCols);
         give_back(w, w.ctl->small_empty, w.small);
+    }
+    if constexpr (kMode == kGram) {
+        if (t.cut < p.cuts - 1) {
+            put_share<0>(p, t, w, w.half * kCols, sum);
+            put_share<32>(p, t, w, w.half * kCols + 32, sum);
+            return true;
+        }
+        if (p.cuts > 1) {
+            if (!wait_shares(p, t, w)) return false;
+            add_shares<0>(p, t, w, w.half * kCols, sum);
+            add_shares<32>(p, t, w, w.half * kCols + 32, sum);
+        }
     }
 #pragma unroll
     for (int c = 0; c < kChunks; ++c) {
@@ -501,6 +569,16 @@ __device__ __forceinline__ bool ortho_epilogue(const OrthoParams& p, const Ortho
         ptx::tmem_ld_wait();
         if (c == kChunks - 1) give_back(w, w.ctl->acc_empty, w.acc);
         const int c0 = col0 + c * 32;
+        if constexpr (kMode == kGram && kWidth == kTile) {           // (wider tiles are not cut)
+            if (t.cut < p.cuts - 1) {
+                put_share<0>(p, t, w, w.half * kCols + c * 32, v);
+                continue;
+            }
+            if (p.cuts > 1) {
+                if (c == 0 && !wait_shares(p, t, w)) return false;
+                add_shares<0>(p, t, w, w.half * kCols + c * 32, v);
+            }
+        }
         if (below || c0 >= ld || row0 >= rows) continue;
         // 2^24 times the sum as it comes; 2^12 as it is held
         if (last) {
@@ -639,17 +717,18 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
     int32_t* status_word = p.status_word;
     pdl_wait();
     const bool skip = status_word != nullptr && *reinterpret_cast<volatile int32_t*>(status_word) != 0;
-    const uint32_t total = (uint32_t)p.steps * (2 * p.sym_tiles + p.step_tiles) * (uint32_t)p.count;
+    const uint32_t total = (uint32_t)p.steps * ((uint32_t)(p.cuts + 1) * p.sym_tiles + p.step_tiles) * (uint32_t)p.count;
 
-    // the item in the ring's next place, for the warps that do not draw; false where a wait ran out
-    auto next_item = [&](uint32_t n, uint32_t& q, bool free_place = true) {
+    // the item in the ring's next place, for the warps that do not draw; false behind the last one, and where a wait ran out
+    auto next_item = [&](uint32_t n, OrthoItem& t, bool free_place = true) {
         const uint32_t s = n % kItems;
         bool ok = ptx::mbar_wait(ptx::smem_addr(&ctl->item_full[s]), (n / kItems) & 1u, abort_flag, status_word);
         ok = __all_sync(0xffffffffu, ok);
-        q = *reinterpret_cast<volatile uint32_t*>(&ctl->item[s]);
+        const int4 a = ctl->item[s][0], b = ctl->item[s][1];
+        t = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
         __syncwarp();
         if (free_place && lane == 0) ptx::mbar_arrive(ptx::smem_addr(&ctl->item_empty[s]));
-        return ok;
+        return ok && t.need >= 0;
     };
 
     if (skip) {
@@ -659,10 +738,8 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
         uint32_t it = 0;
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
-            uint32_t q;
-            ok = next_item(n, q);
-            if (!ok || q >= total) break;
-            const OrthoItem t = ortho_item<kWidth>(p, q);
+            OrthoItem t;
+            if (!next_item(n, t)) break;
             // which operands are read across: both of a tall matrix's A (its reduction runs down X), X of a wide one's step
             const bool across_a = t.mode == kGram && p.tall, across_b = across_a || (t.mode == kStep && !p.tall);
             const bool a_is_x = t.mode == kGram || (t.mode == kStep && p.tall), b_is_x = t.mode == kGram || (t.mode == kStep && !p.tall);
@@ -671,9 +748,10 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
             const int x_first = (t.step & 1) * 2, s_first = t.mode == kStep ? p.b_plane : 0;
             const int za = (a_is_x ? x_first : s_first) * p.count + t.matrix, zb = (b_is_x ? x_first : s_first) * p.count + t.matrix;
             const bool with_extras = !kExact && t.mode == kStep;
-            const int blocks = t.mode == kGram ? p.gram_blocks : p.m_blocks + (with_extras ? step_extras<kWidth>(p) : 0);
+            int from;
+            const int blocks = ortho_blocks(p, t, from) + (with_extras ? step_extras<kWidth>(p) : 0);
             for (int k = 0; k < blocks && ok; ++k, ++it) {
-                const OrthoBlock blk = with_extras ? step_block<kWidth>(p, t, k) : OrthoBlock{k, 0, 0, 0};
+                const OrthoBlock blk = with_extras ? step_block<kWidth>(p, t, k) : OrthoBlock{from + k, 0, 0, 0};
                 const int y = blk.at * kDeep;
                 const uint32_t s = it % kStages;
                 ok = ptx::mbar_wait(ptx::smem_addr(&ctl->empty[s]), ((it / kStages) & 1u) ^ 1u, abort_flag, status_word);
@@ -720,13 +798,12 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
         Turns acc, small;
         bool ok = true;
         for (uint32_t n = 0; ok; ++n) {
-            uint32_t q;
-            ok = next_item(n, q);
-            if (!ok || q >= total) break;
-            const OrthoItem t = ortho_item<kWidth>(p, q);
+            OrthoItem t;
+            if (!next_item(n, t)) break;
             const bool across_a = t.mode == kGram && p.tall, across_b = across_a || (t.mode == kStep && !p.tall);
             const bool with_extras = !kExact && t.mode == kStep;
-            const int blocks = t.mode == kGram ? p.gram_blocks : p.m_blocks + (with_extras ? step_extras<kWidth>(p) : 0);
+            int from;
+            const int blocks = ortho_blocks(p, t, from) + (with_extras ? step_extras<kWidth>(p) : 0);
             const uint32_t idesc = ptx::umma_idesc_f16(kTile, kWidth, across_a, across_b);
             const uint32_t a_step = (across_a ? kUmmaDeep * kRow : kUmmaDeep * 2u) >> 4, b_step = (across_b ? kUmmaDeep * kRow : kUmmaDeep * 2u) >> 4;
             const uint32_t a_lo = ptx::umma_desc_lo(ring, across_a ? kHalfOperand : 16u);
@@ -784,13 +861,16 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
             uint32_t q = 0;
             if (lane == 0) q = atomicAdd(p.drawn, 1u);
             q = __shfl_sync(0xffffffffu, q, 0);
-            if (q < total && lane == 0) {
-                const OrthoItem t = ortho_item<kWidth>(p, q);
-                ok = wait_done(p.done + t.matrix, t.need, abort_flag, status_word);
+            OrthoItem t = {};
+            t.need = -1;
+            if (q < total) {
+                t = ortho_item<kWidth>(p, q);
+                if (lane == 0) ok = wait_done(p.done + t.matrix, t.need, abort_flag, status_word);
+                if (!__all_sync(0xffffffffu, ok)) break;
             }
-            if (!__all_sync(0xffffffffu, ok)) break;
             if (lane == 0) {
-                *reinterpret_cast<volatile uint32_t*>(&ctl->item[slot]) = q;
+                ctl->item[slot][0] = make_int4(t.step, t.mode, t.matrix, t.i);
+                ctl->item[slot][1] = make_int4(t.j, t.tile, t.cut, t.need);
                 ptx::mbar_arrive(ptx::smem_addr(&ctl->item_full[slot]));
             }
             if (q >= total) break;
@@ -800,14 +880,15 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
         // Tells the other blocks of a finished tile: a fence waits until its stores have arrived, 1.5 us, which the epilogue warps
         // would otherwise spend.  An item's place in the ring is only freed then, so that no barrier here is passed twice.
         for (uint32_t n = 0;; ++n) {
-            uint32_t q;
-            if (!next_item(n, q, false) || q >= total) break;
-            const OrthoItem t = ortho_item<kWidth>(p, q);
+            OrthoItem t;
+            if (!next_item(n, t, false)) break;
             bool ok = ptx::mbar_wait(ptx::smem_addr(&ctl->stored[n % kItems]), (n / kItems) & 1u, abort_flag, status_word);
             if (!__all_sync(0xffffffffu, ok)) break;
             if (lane == 0) {
                 asm volatile("fence.proxy.async;\n\tfence.acq_rel.gpu;" ::: "memory");
                 asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.done + t.matrix) : "memory");
+                if (t.mode == kGram && t.cut < p.cuts - 1)
+                    asm volatile("red.release.gpu.global.add.s32 [%0], 1;" ::"l"(p.shares + (int64_t)t.matrix * p.sym_tiles + t.tile) : "memory");
                 ptx::mbar_arrive(ptx::smem_addr(&ctl->item_empty[n % kItems]));
             }
             __syncwarp();
@@ -823,9 +904,8 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
         w.half = (warp - kFirstEpilogueWarp) >> 2;
         w.tmem = tmem + ((uint32_t)(w.quad * 32) << 16);
         for (uint32_t n = 0;; ++n) {
-            uint32_t q;
-            if (!next_item(n, q) || q >= total) break;
-            const OrthoItem t = ortho_item<kWidth>(p, q);
+            OrthoItem t;
+            if (!next_item(n, t)) break;
             bool ok;
             if constexpr (kExact) {
                 ok = t.mode == kGram   ? ortho_epilogue_exact<kGram>(p, t, w)
@@ -859,14 +939,14 @@ __device__ __forceinline__ void inverse_norm(double norm, float& power, float& f
 
 // ---- the start: momentum, the norm, the two fp16 numbers of U / (|U| + eps) ----
 constexpr int kStartThreads = 256;
-constexpr int kStartBlocksMost = 64;                                 // blocks a matrix
+constexpr int kStartBlocks = 8 * kNumSMs;                            // of all matrices, about
 
 struct StartParams {
     const float* G;
     float* momentum;                 // nullable
     double* partial;                 // [count][blocks]: sums of squares
-    uint32_t* drawn;                 // the products' counters, cleared here
-    int32_t* done;
+    uint32_t* counters;              // the products', cleared here: one, `count`, and a few a matrix
+    int counters_each;
     __half* X;
     int64_t x_plane, elements;       // of a matrix: with pitch, without
     int count, rows, cols, ldx, blocks, nesterov;
@@ -887,9 +967,10 @@ __global__ void __launch_bounds__(kStartThreads) ortho_norm_kernel(const StartPa
     pdl_wait();
     if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
     const int matrix = blockIdx.y;
-    if (blockIdx.x == 0 && threadIdx.x == 0) {
-        p.done[matrix] = 0;
-        if (matrix == 0) *p.drawn = 0u;
+    if (blockIdx.x == 0) {
+        if (threadIdx.x == 0) p.counters[1 + matrix] = 0u;
+        if (threadIdx.x == 1 && matrix == 0) p.counters[0] = 0u;
+        for (int i = threadIdx.x; i < p.counters_each; i += kStartThreads) p.counters[1 + p.count + matrix * p.counters_each + i] = 0u;
     }
     const int64_t base = (int64_t)matrix * p.elements;
     double s = 0.0;
@@ -939,8 +1020,16 @@ __global__ void __launch_bounds__(kStartThreads) ortho_scale_kernel(const StartP
     pdl_wait();
     if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
     const int matrix = blockIdx.y;
+    __shared__ double part[kStartThreads / 32];
     double s = 0.0;
-    for (int b = 0; b < p.blocks; ++b) s += p.partial[(int64_t)matrix * p.blocks + b];
+    for (int b = threadIdx.x; b < p.blocks; b += kStartThreads) s += p.partial[(int64_t)matrix * p.blocks + b];
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
+    if ((threadIdx.x & 31) == 0) part[threadIdx.x >> 5] = s;
+    __syncthreads();
+    s = 0.0;
+#pragma unroll
+    for (int w = 0; w < kStartThreads / 32; ++w) s += part[w];
     const double norm = sqrt(s) + p.eps;
     float power, factor;
     inverse_norm(norm, power, factor);
@@ -1396,9 +1485,10 @@ bool plane_map(CUtensorMap* map, const __half* base, int64_t planes, int64_t row
 
 struct OrthoLayout {
     int64_t m, ldx, ldm, x_plane, s_plane;
-    int s_planes, b_plane, start_blocks;
+    int s_planes, b_plane, start_blocks, width, cuts;
+    uint32_t sym_tiles;
     bool exact;
-    size_t S, diag_a, diag_b, partial, counters, bytes;      // offsets behind the planes of X
+    size_t S, diag_a, diag_b, partial, counters, share, bytes;       // offsets behind the planes of X
 };
 OrthoLayout ortho_layout(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols) {
     OrthoLayout l;
@@ -1411,14 +1501,27 @@ OrthoLayout ortho_layout(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols
     l.b_plane = l.exact ? 2 : 1;
     l.x_plane = rows * l.ldx;
     l.s_plane = l.m * l.ldm;
-    const int64_t want = (rows * cols / 4 + 4 * kStartThreads - 1) / (4 * kStartThreads);
-    l.start_blocks = (int)(want < 1 ? 1 : want < kStartBlocksMost ? want : kStartBlocksMost);
+    const int64_t want = (rows * cols / 4 + 4 * kStartThreads - 1) / (4 * kStartThreads), most = kStartBlocks / count > 1 ? kStartBlocks / count : 1;
+    l.start_blocks = (int)(want < 1 ? 1 : want < most ? want : most);
+    // 256 wide tiles take half as much of their operands from the L2 for a product (12 x 768 x 768: 265 us, 285 with 128), where there
+    // are tiles for all SMs
+    l.width = !l.exact && (rows + kTile - 1) / kTile * ((cols + kTile - 1) / kTile) * count > kNumSMs ? 256 : 128;
+    const uint32_t tiles = (uint32_t)((l.m + kTile - 1) / kTile), wide = (uint32_t)((l.m + l.width - 1) / l.width), f = (uint32_t)l.width / kTile;
+    l.sym_tiles = f * wide * (wide + 1) / 2 - (f * wide - tiles);
+    // A's tiles are few, and their reduction is the longer side: it is cut into up to four shares of eight blocks at least while the
+    // SMs have room for them
+    const int64_t blocks = ((rows > cols ? rows : cols) + kDeep - 1) / kDeep;
+    l.cuts = 1;
+    // (waiting for the other shares costs some 4 us: 1024 x 1024, 16 blocks, 165 us whole and 217 cut in bf16, 289 and 309 in fp32;
+    // 1024 x 4096 422 and 302 in bf16, 568 and 408 in fp32)
+    while (l.width == kTile && blocks * (l.exact ? 2 : 1) >= 48 && l.cuts < 4 && (int64_t)(l.cuts + 1) * l.sym_tiles * count <= kNumSMs && blocks / (l.cuts + 1) >= 8) ++l.cuts;
     l.S = up((size_t)(4 * count * l.x_plane) * 2);
     l.diag_a = l.S + up((size_t)(l.s_planes * count * l.s_plane) * 2);
     l.diag_b = l.diag_a + up((size_t)(count * l.ldm) * 4);
     l.partial = l.diag_b + up((size_t)(count * l.ldm) * 4);
     l.counters = l.partial + up((size_t)count * l.start_blocks * 8);
-    l.bytes = l.counters + up((size_t)(count + 1) * 4);
+    l.share = l.counters + up((size_t)(1 + count + (l.cuts > 1 ? count * l.sym_tiles : 0)) * 4);
+    l.bytes = l.share + (size_t)(l.cuts - 1) * count * l.sym_tiles * kTile * kTile * 4;
     return l;
 }
 
@@ -1426,11 +1529,10 @@ template <bool kExact, int kWidth>
 cudaError_t launch_products(const CUtensorMap& x_rows, const CUtensorMap& x_across, const CUtensorMap& s_rows, OrthoParams& p, cudaStream_t stream) {
     const cudaError_t e = opt_in_dynamic_smem<ortho_kernel<kExact, kWidth>>((int)kOrthoSmem);
     if (e != cudaSuccess) return e;
-    const uint32_t tiles = (uint32_t)((p.m + kTile - 1) / kTile), wide = (uint32_t)((p.m + kWidth - 1) / kWidth);
-    p.sym_tiles = kWidth / kTile * wide * (wide + 1) / 2 - (kWidth / kTile * wide - tiles);
     p.step_cols = (uint32_t)((p.cols + kWidth - 1) / kWidth);
     p.step_tiles = (uint32_t)((p.rows + kTile - 1) / kTile) * p.step_cols;
-    const int64_t most = (int64_t)p.count * (p.step_tiles > p.sym_tiles ? p.step_tiles : p.sym_tiles);
+    const uint32_t grams = p.sym_tiles * (uint32_t)p.cuts;
+    const int64_t most = (int64_t)p.count * (p.step_tiles > grams ? p.step_tiles : grams);
     return launch_pdl(ortho_kernel<kExact, kWidth>, dim3((unsigned)(most < kNumSMs ? most : kNumSMs)), dim3(ortho_threads(kExact)), kOrthoSmem, stream,
                       x_rows, x_across, s_rows, p);
 }
@@ -1476,10 +1578,10 @@ size_t orthogonalize_workspace_bytes(sbp_dtype dt, int64_t count, int64_t rows, 
     return ortho_small_slice(rows, cols) > 0 ? 256 : ortho_layout(dt, count, rows, cols).bytes;
 }
 
-// the items of a launch (three products of at most this many tiles, up to 32 times) and the planes a tensor map counts are 32-bit numbers
+// the items of a launch (A's in four shares, two more products of at most this many tiles, up to 32 times) and the planes a tensor map counts are 32-bit numbers
 bool orthogonalize_supported(int64_t count, int64_t rows, int64_t cols) {
     const int64_t tiles = (rows + kTile - 1) / kTile * ((cols + kTile - 1) / kTile);
-    return rows <= (1 << 16) && cols <= (1 << 16) && count <= (1 << 16) - 1 && 3 * 32 * tiles * count < (1ll << 31);
+    return rows <= (1 << 16) && cols <= (1 << 16) && count <= (1 << 16) - 1 && 6 * 32 * tiles * count < (1ll << 31);
 }
 
 cudaError_t launch_orthogonalize(sbp_dtype dt, const float* G, float* momentum, float beta, bool nesterov, int64_t count, int64_t rows, int64_t cols,
@@ -1493,8 +1595,8 @@ cudaError_t launch_orthogonalize(sbp_dtype dt, const float* G, float* momentum, 
     s.momentum = momentum;
     s.partial = reinterpret_cast<double*>(ws + l.partial);
     s.X = reinterpret_cast<__half*>(ws);
-    s.drawn = reinterpret_cast<uint32_t*>(ws + l.counters);
-    s.done = reinterpret_cast<int32_t*>(ws + l.counters) + 1;
+    s.counters = reinterpret_cast<uint32_t*>(ws + l.counters);
+    s.counters_each = l.cuts > 1 ? (int)l.sym_tiles : 0;
     s.x_plane = l.x_plane;
     s.elements = rows * cols;
     s.count = (int)count;
@@ -1538,11 +1640,14 @@ cudaError_t launch_orthogonalize(sbp_dtype dt, const float* G, float* momentum, 
     p.m_blocks = (int)((l.m + kDeep - 1) / kDeep);
     p.steps = steps;
     p.out = O;
-    p.drawn = s.drawn;
-    p.done = s.done;
+    p.sym_tiles = l.sym_tiles;
+    p.cuts = l.cuts;
+    p.drawn = s.counters;
+    p.done = reinterpret_cast<int32_t*>(s.counters) + 1;
+    p.shares = p.done + count;
+    p.share = reinterpret_cast<float4*>(ws + l.share);
     if (l.exact) return launch_products<true, 128>(x_rows, x_across, s_rows, p, stream);
-    return (rows + kTile - 1) / kTile * ((cols + kTile - 1) / kTile) * count > kNumSMs ? launch_products<false, 256>(x_rows, x_across, s_rows, p, stream)
-                                                                                       : launch_products<false, 128>(x_rows, x_across, s_rows, p, stream);
+    return l.width == 256 ? launch_products<false, 256>(x_rows, x_across, s_rows, p, stream) : launch_products<false, 128>(x_rows, x_across, s_rows, p, stream);
 }
 
 }  // namespace sbp
