@@ -285,10 +285,14 @@ __global__ void __launch_bounds__(norm_backward_threads(kNV * Vec<T>::N, kMany),
         f32x2 pre1[E2], pre0[E2], S1[E2], S0[E2];
 #pragma unroll
         for (int e = 0; e < E2; ++e) pre1[e] = pre0[e] = S1[e] = S0[e] = none;
-        uint32_t first = 0, last = 0, cur = 0;
+        // the gate rows of the first and the last entry, and that of the rows in S1 and S0 (kNoGate before there is one: entries outside
+        // the tensor have none)
+        constexpr uint32_t kNoGate = 0xffffffffu;
+        uint32_t first = kNoGate, last = kNoGate, cur = p.gate != nullptr ? kNoGate : 0u;
         if (p.gate != nullptr && lo < hi) {
-            first = cur = p.gate_group((uint32_t)mapped_row(p.keep_rows, lo) & 0x7fffffffu);
-            last = p.gate_group((uint32_t)mapped_row(p.keep_rows, hi - 1) & 0x7fffffffu);
+            const int32_t a = mapped_row(p.keep_rows, lo), b = mapped_row(p.keep_rows, hi - 1);
+            if (a >= 0 && a < p.M) first = p.gate_group((uint32_t)a);
+            if (b >= 0 && b < p.M) last = p.gate_group((uint32_t)b);
         }
         auto accumulate = [&](float4* a, const f32x2* f, bool old) {     // into shared memory (old: or a row of memory)
             const float2 u = both(f[0]), v = both(f[1]);
@@ -297,6 +301,7 @@ __global__ void __launch_bounds__(norm_backward_threads(kNV * Vec<T>::N, kMany),
             *a = s;
         };
         auto put_gate = [&]() {                           // the end of a gate row (or, without a gate, of the list): S1 and S0 go where they belong
+            if (cur == kNoGate) return;
             const bool partial = cur == first || cur == last;
             float* to = partial ? p.gate_sums + (worker * 2 + (cur == first ? 0 : 1)) * C : p.dgate + (int64_t)cur * C;
 #pragma unroll
@@ -601,7 +606,7 @@ struct NormReduceParams {
     float* out[kNormSums];
     float* dgate;                                     // of several rows, else nullptr
     const int32_t *keep_rows, *M_keep_dev, *status_word;
-    int64_t M_keep_cap, workers, gate_group, gate_rows;
+    int64_t M, M_keep_cap, workers, gate_group, gate_rows;
     int C, accumulate, blocks, few_workers, tiles, gate_tiles;       // column tiles of a sum / of a gate row
     int outputs, output[kNormSums];                                  // which of the sums are wanted
 };
@@ -646,8 +651,8 @@ __global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormR
             start = 0;
         }
         if (group < p.gate_rows) {
-            // the kept rows [a, b) of this gate row, and the workers that had them
-            const int64_t r0 = group * p.gate_group, r1 = r0 + p.gate_group;
+            // the kept rows [a, b) of this gate row (without entries past the tensor), and the workers that had them
+            const int64_t r0 = group * p.gate_group, r1 = r0 + p.gate_group < p.M ? r0 + p.gate_group : p.M;
             int64_t a, b;
             if (p.keep_rows == nullptr) {
                 a = r0 < M_keep ? r0 : M_keep;
@@ -854,6 +859,7 @@ cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR,
     p.M_keep_cap = M_keep_cap;
     p.dgate = dgate;
     p.want = (dpost_w ? 1 : 0) | (dpost_b ? 2 : 0) | (dpre_w ? 4 : 0) | (dpre_b ? 8 : 0) | (dgate ? 16 : 0);
+    if (gate_group > M) gate_group = M;
     const int64_t gate_rows = dgate != nullptr ? (M + gate_group - 1) / gate_group : 0;
     p.one_gate = gate_rows == 1;
     int sums = 0;
@@ -892,6 +898,7 @@ cudaError_t launch_block_norm_backward(sbp_dtype dt, bool layer, const void* dR,
     r.keep_rows = keep_rows;
     r.M_keep_dev = M_keep_dev;
     r.status_word = status_word;
+    r.M = M;
     r.M_keep_cap = M_keep_cap;
     r.workers = p.workers;
     r.gate_group = gate_group;

@@ -187,6 +187,25 @@ def test_counts_on_the_device_accumulation_and_in_place(dtype, C):
     check_backward(dtype, 0, full, o, backward64(full, 0, keep, 1.0), keep)
 
 
+@pytest.mark.parametrize("dtype,C", [("bf16", 64), ("bf16", 768), ("f32", 1032)])
+@pytest.mark.parametrize("group", [1, 13, 300, 2 ** 62])
+def test_entries_outside_the_tensor_are_skipped(dtype, C, group):
+    M, keep = 300, 120
+    s = inputs(dtype, M, C, keep, True, True, min(group, M))
+    s["group"] = group
+    s["rows"][:5] = torch.tensor([-2 ** 31, -7, -3, -2, -1], dtype=torch.int32)
+    s["rows"][100:] = torch.arange(M, M + 20, dtype=torch.int32)
+    s["rows"][-1] = 2 ** 31 - 1
+    o = run_backward(dtype, 0, s, M, C, keep)
+    inner = slice(5, 100)
+    some = dict(s, rows=s["rows"][inner].contiguous(), dZ=s["dZ"][inner], R=s["R"][inner], Yk=s["Yk"][inner], group=min(group, M))
+    want = backward64(some, 0, 95, 0.9)
+    check_backward(dtype, 0, some, dict(o, dY=o["dY"][inner]), want, 95)
+    assert not o["dY"][:5].any() and not o["dY"][100:].any()
+    f = run_forward(dtype, 0, s, M, C, keep)
+    assert torch.equal(f["R_keep"][inner], f["R"][some["rows"].long()])
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
 def test_no_rows_kept(dtype):
     M, C = 40, 136
