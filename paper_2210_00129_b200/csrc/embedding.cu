@@ -381,45 +381,66 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumParams p) {
     if (cur < V) put(true);
 }
 
-// Adds the partial rows of the ids that cross a piece's border: the block of the piece in which such an id begins.  Eight warps
-// take the pieces in turns, and their sums are added in the order of the warps.
+// Adds the partial rows of the ids that cross a piece's border.  A warp looks after one strip of the piece in which such an id begins and
+// adds up the pieces itself, in their order, where they are kJoinAlone at most; a longer one - of which no two begin in a block's
+// eight pieces - is left to all of the block's warps, who take its pieces in turns and whose sums are added in the order of the
+// warps.  (A block for each piece: 8 blocks an SM that mostly find nothing to do.)
+constexpr int kJoinAlone = 16;
 template <typename T>
 __global__ void __launch_bounds__(256) embedding_join_kernel(const SumParams p) {
     constexpr int N = Vec<T>::N, P = N / 2;
     __shared__ f32x2 part[8][32][P + 1];
+    __shared__ int64_t long_piece, long_end;
     pdl_launch_dependents();
     pdl_wait();
-    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap);
-    const int64_t piece = blockIdx.x / p.strips, lo = piece * p.piece, hi = lo + p.piece;
-    if (hi >= n) return;
-    const uint32_t k = p.keys[hi - 1];
-    if (k >= (uint32_t)p.V || p.keys[hi] != k || (lo > 0 && p.keys[lo - 1] == k)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t pieces = (n + p.piece - 1) / p.piece;
-    // pieces [piece + 1, end) begin with this id (the list is sorted: 32 probes a step)
-    int64_t end = piece + 2, top = pieces;
-    while (end < top) {
-        const int64_t step = (top - end + 31) / 32, at = end + lane * step;
-        const int same = __popc(__ballot_sync(0xffffffffu, at < top && p.keys[(at < top ? at : end) * p.piece] == k));
-        if (same == 0) break;
-        const int64_t last = end + (same - 1) * step;
-        end = last + 1;
-        top = last + step < top ? last + step : top;
-    }
+    if (threadIdx.x == 0) long_piece = -1;
+    __syncthreads();
+    const int64_t n = load_m_keep(p.M_keep_dev, p.M_keep_cap);
+    const int64_t piece = blockIdx.x / p.strips * 8 + warp, lo = piece * p.piece, hi = lo + p.piece;
     const int v = (int)(blockIdx.x % p.strips) * 32 + lane;
     const int64_t C = (int64_t)p.vecs * N;
     f32x2 acc[P];
+    // pieces from, from + step, ... of the id that begins in piece `first`
+    auto add_pieces = [&](int64_t first, int64_t from, int64_t end, int64_t step) {
 #pragma unroll
-    for (int e = 0; e < P; ++e) acc[e] = pair(0.f, 0.f);
-    if (v < p.vecs) {
+        for (int e = 0; e < P; ++e) acc[e] = pair(0.f, 0.f);
+        if (v >= p.vecs) return;
 #pragma unroll 4
-        for (int64_t q = piece + warp; q < end; q += 8) {
+        for (int64_t q = from; q < end; q += step) {
             f32x2 f[P];
-            load_f32<N>(p.partial + (q * 2 + (q == piece ? 1 : 0)) * C + (int64_t)v * N, f);
+            load_f32<N>(p.partial + (q * 2 + (q == first ? 1 : 0)) * C + (int64_t)v * N, f);
 #pragma unroll
             for (int e = 0; e < P; ++e) acc[e] = add(acc[e], f[e]);
         }
+    };
+    if (hi < n) {
+        const uint32_t k = p.keys[hi - 1];
+        if (k < (uint32_t)p.V && p.keys[hi] == k && (lo == 0 || p.keys[lo - 1] != k)) {
+            const int64_t pieces = (n + p.piece - 1) / p.piece;
+            // pieces [piece + 1, end) begin with this id (the list is sorted: 32 probes a step)
+            int64_t end = piece + 2, top = pieces;
+            while (end < top) {
+                const int64_t step = (top - end + 31) / 32, at = end + lane * step;
+                const int same = __popc(__ballot_sync(0xffffffffu, at < top && p.keys[(at < top ? at : end) * p.piece] == k));
+                if (same == 0) break;
+                const int64_t last = end + (same - 1) * step;
+                end = last + 1;
+                top = last + step < top ? last + step : top;
+            }
+            if (end - piece <= kJoinAlone) {
+                add_pieces(piece, piece, end, 1);
+                if (v < p.vecs) put_sum(p.dTable + (int64_t)k * C + (int64_t)v * N, acc, p.scale, p.accumulate != 0);
+            } else if (lane == 0) {
+                long_piece = piece;
+                long_end = end;
+            }
+        }
     }
+    __syncthreads();
+    const int64_t first = long_piece;
+    if (first < 0) return;
+    add_pieces(first, first + warp, long_end, 8);
 #pragma unroll
     for (int e = 0; e < P; ++e) part[warp][lane][e] = acc[e];
     __syncthreads();
@@ -428,7 +449,7 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumParams p) 
     for (int w = 1; w < 8; ++w)
 #pragma unroll
         for (int e = 0; e < P; ++e) acc[e] = add(acc[e], part[w][lane][e]);
-    put_sum(p.dTable + (int64_t)k * C + (int64_t)v * N, acc, p.scale, p.accumulate != 0);
+    put_sum(p.dTable + (int64_t)p.keys[(first + 1) * p.piece] * C + (int64_t)v * N, acc, p.scale, p.accumulate != 0);
 }
 
 // ---- backward: short lists ----
@@ -689,7 +710,7 @@ cudaError_t launch_embedding_backward(sbp_dtype dt, const void* dOut, bool compa
     s.accumulate = accumulate;
     s.scale = scale;
     const int64_t warps = su.pieces * su.strips;
-    const dim3 sum_grid((unsigned)((warps + 7) / 8)), join_grid((unsigned)warps);
+    const dim3 sum_grid((unsigned)((warps + 7) / 8)), join_grid((unsigned)((su.pieces + 7) / 8 * su.strips));
     e = dt == SBP_BF16 ? launch_pdl(embedding_sum_kernel<__nv_bfloat16>, sum_grid, dim3(256), 0, stream, s)
                        : launch_pdl(embedding_sum_kernel<float>, sum_grid, dim3(256), 0, stream, s);
     if (e != cudaSuccess || su.pieces < 2) return e;
