@@ -1503,9 +1503,10 @@ OrthoLayout ortho_layout(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols
     l.s_plane = l.m * l.ldm;
     const int64_t want = (rows * cols / 4 + 4 * kStartThreads - 1) / (4 * kStartThreads), most = kStartBlocks / count > 1 ? kStartBlocks / count : 1;
     l.start_blocks = (int)(want < 1 ? 1 : want < most ? want : most);
-    // 256 wide tiles take half as much of their operands from the L2 for a product (12 x 768 x 768: 265 us, 285 with 128), where there
-    // are tiles for all SMs
-    l.width = !l.exact && (rows + kTile - 1) / kTile * ((cols + kTile - 1) / kTile) * count > kNumSMs ? 256 : 128;
+    // 256 wide tiles take half as much of their operands from the L2 for a product, but there are half as many: from about three 128
+    // wide ones an SM on (4 x 2048 x 2048, 1024 of them: 730 us, 833 with 128; 512: 499 and 537; 24 x 768 x 768, 864: 374 and 394;
+    // 12 x 768 x 768, 432: 237 and 222; 4 x 2304 x 768, 432: 274 and 229; 8 x 1261 x 222, 160: 226 and 189)
+    l.width = !l.exact && (rows + kTile - 1) / kTile * ((cols + kTile - 1) / kTile) * count > 3 * kNumSMs ? 256 : 128;
     const uint32_t tiles = (uint32_t)((l.m + kTile - 1) / kTile), wide = (uint32_t)((l.m + l.width - 1) / l.width), f = (uint32_t)l.width / kTile;
     l.sym_tiles = f * wide * (wide + 1) / 2 - (f * wide - tiles);
     // A's tiles are few, and their reduction is the longer side: it is cut into up to four shares of eight blocks at least while the

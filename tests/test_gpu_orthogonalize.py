@@ -92,7 +92,8 @@ def check(dtype, O, U, steps=5, eps=1e-7, scale=1.0):
 SIZES = [(1, 1, 1), (1, 1, 100), (2, 100, 1), (3, 8, 8), (2, 5, 13), (1, 64, 64), (1, 100, 257), (2, 128, 128), (1, 129, 200), (2, 136, 136),
          (1, 256, 512), (1, 512, 256), (1, 300, 300), (2, 200, 1000), (1, 1000, 136), (1, 768, 768), (3, 384, 640), (1, 2304, 768), (40, 130, 140),
          (1, 131, 4099), (1, 128, 2048), (2, 2048, 128), (1, 100, 513), (3, 64, 1000), (1, 17, 129), (1, 260, 60), (2, 3, 1500), (1, 128, 2049),
-         (1, 2100, 24), (200, 40, 300), (1, 520, 2100), (2, 1500, 260), (1, 3000, 140)]
+         (1, 2100, 24), (200, 40, 300), (1, 520, 2100), (2, 1500, 260), (1, 3000, 140),
+         (28, 500, 440), (30, 440, 500), (57, 264, 300)]
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
