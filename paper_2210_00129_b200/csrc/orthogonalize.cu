@@ -986,16 +986,23 @@ __global__ void __launch_bounds__(kStartThreads) ortho_norm_kernel(const StartPa
     if constexpr (kVec) {
         const float4* G = reinterpret_cast<const float4*>(p.G + base);
         float4* mom = p.momentum != nullptr ? reinterpret_cast<float4*>(p.momentum + base) : nullptr;
-#pragma unroll 4
-        for (int64_t i = (int64_t)blockIdx.x * kStartThreads + threadIdx.x; i < p.elements / 4; i += stride) {
-            const float4 g = __ldg(G + i);
-            float4 m = make_float4(0.f, 0.f, 0.f, 0.f);
-            if (mom != nullptr) m = mom[i];
-            one(g.x, m.x);
-            one(g.y, m.y);
-            one(g.z, m.z);
-            one(g.w, m.w);
-            if (mom != nullptr) mom[i] = m;
+        constexpr int kBatch = 4;                     // loads of a thread before its stores, which might be to the same places for all it knows
+        for (int64_t i = (int64_t)blockIdx.x * kStartThreads + threadIdx.x; i < p.elements / 4; i += kBatch * stride) {
+            float4 g[kBatch], m[kBatch];
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                const bool in = i + u * stride < p.elements / 4;
+                g[u] = in ? __ldg(G + i + u * stride) : make_float4(0.f, 0.f, 0.f, 0.f);
+                m[u] = in && mom != nullptr ? mom[i + u * stride] : make_float4(0.f, 0.f, 0.f, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < kBatch; ++u) {
+                one(g[u].x, m[u].x);
+                one(g[u].y, m[u].y);
+                one(g[u].z, m[u].z);
+                one(g[u].w, m[u].w);
+                if (mom != nullptr && i + u * stride < p.elements / 4) mom[i + u * stride] = m[u];
+            }
         }
     } else {
         for (int64_t i = (int64_t)blockIdx.x * kStartThreads + threadIdx.x; i < p.elements; i += stride) {
