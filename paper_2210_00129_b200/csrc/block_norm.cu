@@ -612,16 +612,38 @@ struct NormReduceParams {
 };
 __device__ __forceinline__ float add_rows(const float* from, int64_t stride, int64_t n) {
     float s = 0.f;
-    int64_t i = 0;
-    for (; i + 8 <= n; i += 8) {
+    for (int64_t i = 0; i < n; i += 8) {              // eight loads together, the last ones too
         float f[8];
 #pragma unroll
-        for (int u = 0; u < 8; ++u) f[u] = __ldg(from + (i + u) * stride);
+        for (int u = 0; u < 8; ++u) f[u] = i + u < n ? __ldg(from + (i + u) * stride) : 0.f;
 #pragma unroll
         for (int u = 0; u < 8; ++u) s += f[u];
     }
-    for (; i < n; ++i) s += __ldg(from + i * stride);
     return s;
+}
+// First positions of the ascending list whose entries are at least value[0], value[1]: two searches as warp_lower_bound's, side by side.
+__device__ __forceinline__ void warp_lower_bounds(const int32_t* rows, int64_t n, const int64_t (&value)[2], int lane, int64_t (&lo)[2]) {
+    int64_t hi[2] = {n, n};
+    lo[0] = lo[1] = 0;
+    while (hi[0] > lo[0] || hi[1] > lo[1]) {
+        bool below[2];
+        int64_t step[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            step[u] = (hi[u] - lo[u] + 31) / 32;
+            const int64_t at = lo[u] + lane * step[u];
+            below[u] = at < hi[u] && (int64_t)__ldg(rows + at) < value[u];
+        }
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int c = __popc(__ballot_sync(0xffffffffu, below[u]));
+            if (hi[u] <= lo[u]) continue;
+            const int64_t last = lo[u] + (c - 1) * step[u];          // below
+            const int64_t end = c == 0 || step[u] == 1 ? 0 : last + step[u];
+            if (c != 0) lo[u] = last + 1;
+            hi[u] = end == 0 ? lo[u] : end < hi[u] ? end : hi[u];
+        }
+    }
 }
 __global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormReduceParams p) {
     __shared__ float part[kReduceThreads];
@@ -653,16 +675,16 @@ __global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormR
         if (group < p.gate_rows) {
             // the kept rows [a, b) of this gate row (without entries past the tensor), and the workers that had them
             const int64_t r0 = group * p.gate_group, r1 = r0 + p.gate_group < p.M ? r0 + p.gate_group : p.M;
-            int64_t a, b;
+            int64_t at[2];
             if (p.keep_rows == nullptr) {
-                a = r0 < M_keep ? r0 : M_keep;
-                b = r1 < M_keep ? r1 : M_keep;
+                at[0] = r0 < M_keep ? r0 : M_keep;
+                at[1] = r1 < M_keep ? r1 : M_keep;
             } else {
-                a = warp_lower_bound(p.keep_rows, M_keep, r0, lane);
-                const int64_t most = a + p.gate_group < M_keep ? p.gate_group : M_keep - a;
-                b = a + warp_lower_bound(p.keep_rows + a, most, r1, lane);
+                const int64_t rows[2] = {r0, r1};
+                warp_lower_bounds(p.keep_rows, M_keep, rows, lane, at);
             }
-            const int64_t w0 = a < b ? a / chunk : 0, w1 = a < b ? (b - 1) / chunk + 1 : 0;
+            const int64_t a = at[0], b = at[1];
+            const int64_t w0 = a < b ? (uint32_t)a / (uint32_t)chunk : 0, w1 = a < b ? (uint32_t)(b - 1) / (uint32_t)chunk + 1 : 0;
             // inside one worker's rows it is already written
             if (!(w1 - w0 == 1 && a > w0 * chunk && b < (w0 + 1) * chunk && b < M_keep)) out = p.dgate + group * p.C;
             // a worker that begins before this gate row has it as its last one, the others as their first

@@ -410,12 +410,20 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumParams p) 
 #pragma unroll
         for (int e = 0; e < P; ++e) acc[e] = pair(0.f, 0.f);
         if (v >= p.vecs) return;
-#pragma unroll 4
-        for (int64_t q = from; q < end; q += step) {
-            f32x2 f[P];
-            load_f32<N>(p.partial + (q * 2 + (q == first ? 1 : 0)) * C + (int64_t)v * N, f);
+        constexpr int kAhead = 4;                     // loads under way together
+        for (int64_t q = from; q < end; q += kAhead * step) {
+            f32x2 f[kAhead][P];
 #pragma unroll
-            for (int e = 0; e < P; ++e) acc[e] = add(acc[e], f[e]);
+            for (int u = 0; u < kAhead; ++u) {
+                const int64_t at = q + u * step;
+#pragma unroll
+                for (int e = 0; e < P; ++e) f[u][e] = pair(0.f, 0.f);
+                if (at < end) load_f32<N>(p.partial + (at * 2 + (at == first ? 1 : 0)) * C + (int64_t)v * N, f[u]);
+            }
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u)
+#pragma unroll
+                for (int e = 0; e < P; ++e) acc[e] = add(acc[e], f[u][e]);
         }
     };
     if (hi < n) {
