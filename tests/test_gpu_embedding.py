@@ -159,3 +159,23 @@ def test_captured_and_replayed_on_another_stream():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(dT, want)
+
+
+@pytest.mark.parametrize("M", [700, 9000])
+def test_calls_at_once_on_three_streams(M):
+    V, C = 5000, 256
+    g = torch.Generator(device="cuda").manual_seed(4)
+    ids = [ids_of(how, M, V, g) for how in ("skewed", "uniform", "one")]
+    dOut = torch.randn((M, C), device="cuda", generator=g).bfloat16()
+    want = [gradient("bf16", dOut, i, None, M, M, V, C) for i in ids]
+    nbytes = sbp.sbp_embedding_backward_workspace_bytes(1, M, V, C)
+    ws = [torch.empty(nbytes, dtype=torch.uint8, device="cuda") for _ in ids]
+    dT = [torch.full_like(w, float("nan")) for w in want]
+    streams = [torch.cuda.Stream() for _ in ids]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for i, w, t, s in zip(ids, ws, dT, streams):
+            with torch.cuda.stream(s):
+                sbp.sbp_embedding_backward(1, dOut, i, None, None, M, M, V, C, 3.0, t, 0, w, nbytes)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(dT, want))

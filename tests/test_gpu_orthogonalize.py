@@ -182,3 +182,20 @@ def test_captured_and_replayed():
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(O, want)
+
+
+@pytest.mark.parametrize("count,rows,cols", [(3, 640, 512), (20, 100, 700)])
+def test_calls_at_once_on_three_streams(count, rows, cols):
+    G = [gradient(how, count, rows, cols) for how in ("normal", "low", "mean")]
+    want = [run("bf16", g) for g in G]
+    nbytes = sbp.sbp_orthogonalize_workspace_bytes(1, count, rows, cols)
+    ws = [torch.empty(nbytes, dtype=torch.uint8, device="cuda") for _ in G]
+    O = [torch.full_like(w, float("nan")) for w in want]
+    streams = [torch.cuda.Stream() for _ in G]
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for g, w, o, s in zip(G, ws, O, streams):
+            with torch.cuda.stream(s):
+                sbp.sbp_orthogonalize(1, g, None, 0.0, count, rows, cols, 5, 1e-7, 1.0, o, 0, w, nbytes)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(O, want))
