@@ -48,7 +48,7 @@ norm_forward_kernel(const NormFwdParams p) {
     __shared__ float4 scratch[kMulti ? 64 : 1];
     pdl_launch_dependents();
     pdl_wait();
-    if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
+    if (block_sees_error(p.status_word)) return;
     const int lane = threadIdx.x & 31;
     const int64_t worker = kMulti ? (int64_t)blockIdx.x : (int64_t)blockIdx.x * (blockDim.x >> 5) + (threadIdx.x >> 5);
     const int64_t workers = kMulti ? (int64_t)gridDim.x : (int64_t)gridDim.x * (blockDim.x >> 5);
@@ -262,7 +262,7 @@ __global__ void __launch_bounds__(norm_backward_threads(kNV * Vec<T>::N, kMany),
     __shared__ float4 scratch[kMulti ? (kMany ? 1 : kNormMostWorkers) * 64 : 1];
     pdl_launch_dependents();
     pdl_wait();
-    if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
+    if (block_sees_error(p.status_word)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int width = kMulti ? p.warps * 32 : kLanes, mine = threadIdx.x / width;          // threads of a worker; which one of the block
     RowThreads<kLanes> row = {(int)threadIdx.x % width, width, p.warps, mine + 1, 0, scratch + mine * 64};
@@ -649,7 +649,7 @@ __global__ void __launch_bounds__(kReduceThreads) norm_reduce_kernel(const NormR
     __shared__ float part[kReduceThreads];
     pdl_launch_dependents();
     pdl_wait();
-    if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
+    if (block_sees_error(p.status_word)) return;
     const int lane = threadIdx.x & 31, slice = threadIdx.x >> 5;
     float *out = nullptr, s = 0.f;
     int64_t c;

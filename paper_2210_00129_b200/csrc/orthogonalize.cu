@@ -716,7 +716,7 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
     volatile int* abort_flag = &ctl->abort_flag;
     int32_t* status_word = p.status_word;
     pdl_wait();
-    const bool skip = status_word != nullptr && *reinterpret_cast<volatile int32_t*>(status_word) != 0;
+    const bool skip = block_sees_error(status_word);
     const uint32_t total = (uint32_t)p.steps * ((uint32_t)(p.cuts + 1) * p.sym_tiles + p.step_tiles) * (uint32_t)p.count;
 
     // the item in the ring's next place, for the warps that do not draw; false behind the last one, and where a wait ran out
@@ -965,7 +965,7 @@ __global__ void __launch_bounds__(kStartThreads) ortho_norm_kernel(const StartPa
     __shared__ double part[kStartThreads / 32];
     pdl_launch_dependents();
     pdl_wait();
-    if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
+    if (block_sees_error(p.status_word)) return;
     const int matrix = blockIdx.y;
     if (blockIdx.x == 0) {
         if (threadIdx.x == 0) p.counters[1 + matrix] = 0u;
@@ -1025,7 +1025,7 @@ __global__ void __launch_bounds__(kStartThreads) ortho_norm_kernel(const StartPa
 __global__ void __launch_bounds__(kStartThreads) ortho_scale_kernel(const StartParams p) {
     pdl_launch_dependents();
     pdl_wait();
-    if (p.status_word != nullptr && *reinterpret_cast<const volatile int32_t*>(p.status_word) != 0) return;
+    if (block_sees_error(p.status_word)) return;
     const int matrix = blockIdx.y;
     __shared__ double part[kStartThreads / 32];
     double s = 0.0;
@@ -1149,9 +1149,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const Sma
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&tmem_slot);
     volatile int* abort_flag = &abort_slot;
     pdl_wait();
-    // (an error that lies before this call is seen by all blocks of the cluster alike, or by none that matter: a block that goes on
-    // alone would wait for the others, so they agree below)
-    const bool skip = p.status_word != nullptr && *reinterpret_cast<volatile int32_t*>(p.status_word) != 0;
+    // (a block that goes on alone would wait for the others of its cluster, so they agree below)
+    const bool skip = block_sees_error(p.status_word);
     bool ok = !skip;
 
     // ---- momentum, norm, X ----

@@ -18,6 +18,15 @@ __device__ __forceinline__ void report_device_error(int32_t* status_word, int32_
     if (status_word != nullptr) atomicCAS(status_word, 0, code);
 }
 
+// Whether the status word holds an earlier error: one answer for the whole block.  The word may change meanwhile (calls on several
+// streams can share it), so that threads reading it for themselves could part, and those that stay would wait at their
+// barriers for the others.  To be called by all threads of a one-dimensional block.
+__device__ __forceinline__ bool block_sees_error(const int32_t* status_word) {
+    if (status_word == nullptr) return false;
+    const int seen = threadIdx.x == 0 && *reinterpret_cast<const volatile int32_t*>(status_word) != 0;
+    return __syncthreads_or(seen) != 0;
+}
+
 // Programmatic dependent launch: every kernel of the library lets its successor start launching
 // right away and itself waits for its predecessor's results before touching global memory, so
 // launch latency and block scheduling overlap with the tail of the previous kernel.
