@@ -235,7 +235,10 @@ size_t sbp_linear_backward_workspace_bytes(sbp_dtype dt, int64_t M, int64_t M_ke
  * workspace: at least sbp_linear_backward_workspace_bytes(...) bytes, 256-byte
  * aligned, used only during the call's kernels (SBP_ERR_WORKSPACE if short).
  * status_word (dev, nullable): must be zero before the call; receives the first
- * device-side error (SBP_ERR_TIMEOUT, SBP_ERR_BAD_INDICES), else stays zero.
+ * device-side error (SBP_ERR_TIMEOUT, SBP_ERR_BAD_INDICES), else stays zero.  Later calls
+ * that are given the word with an error in it leave their outputs alone.  Calls on several
+ * streams may share a word: one that is running while another reports an error may leave
+ * its outputs partly written and take as long as its waits may (2 s).
  * Results are deterministic: every sum is added up in a fixed order.
  */
 sbp_status sbp_linear_backward(sbp_dtype dt,

@@ -339,7 +339,7 @@ __global__ void __launch_bounds__(128 * G, G == 2 ? 2 : 1) attention_bwd_kernel(
     const uint32_t tmem = __shfl_sync(0xffffffffu, *reinterpret_cast<volatile uint32_t*>(&sh.tmem_slot), 0);
     volatile int* abort_flag = &sh.abort_flag;
     pdl_wait();
-    const bool skip_all = p.status_word != nullptr && *reinterpret_cast<volatile int32_t*>(p.status_word) != 0;
+    const bool skip_all = block_sees_error(p.status_word);
 
     const int quad = warp & 3, g = warp >> 2;               // TMEM lane quadrant of this warp; which 64 key columns it takes
     const int row = quad * 32 + lane;                       // accumulator row: a query, or a key in the dV / dK read-out

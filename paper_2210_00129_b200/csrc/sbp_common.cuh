@@ -20,11 +20,14 @@ __device__ __forceinline__ void report_device_error(int32_t* status_word, int32_
 
 // Whether the status word holds an earlier error: one answer for the whole block.  The word may change meanwhile (calls on several
 // streams can share it), so that threads reading it for themselves could part, and those that stay would wait at their
-// barriers for the others.  To be called by all threads of a one-dimensional block.
+// barriers for the others.  To be called once, by all threads of a one-dimensional block.  (Through shared memory: the answer of
+// __syncthreads_or costs the kernels that use every register up to a hundred bytes of spills.)
 __device__ __forceinline__ bool block_sees_error(const int32_t* status_word) {
     if (status_word == nullptr) return false;
-    const int seen = threadIdx.x == 0 && *reinterpret_cast<const volatile int32_t*>(status_word) != 0;
-    return __syncthreads_or(seen) != 0;
+    __shared__ int seen;
+    if (threadIdx.x == 0) seen = *reinterpret_cast<const volatile int32_t*>(status_word);
+    __syncthreads();
+    return *reinterpret_cast<volatile int*>(&seen) != 0;
 }
 
 // Programmatic dependent launch: every kernel of the library lets its successor start launching

@@ -543,7 +543,11 @@ split_products_kernel(const __grid_constant__ SplitParams prm) {
     const uint32_t tmem = *reinterpret_cast<volatile uint32_t*>(&ctl->tmem_slot);
     int32_t* status_word = prm.status_word;
     pdl_wait();
-    const bool skip_all = status_word != nullptr && *reinterpret_cast<volatile int32_t*>(status_word) != 0;
+    bool skip_all = ptx::warp_sees_error(status_word);
+    if (status_word != nullptr) {
+        if (warp < kEpiWarps) skip_all = ptx::bar_or<kEpiBarrier, 32 * kEpiWarps>(skip_all);
+        else if (warp < kMmaWarp) skip_all = ptx::bar_or<kProducerBarrier, kProducers>(skip_all);
+    }
     const int M_keep = (int)load_m_keep(prm.M_keep_dev, prm.M_keep_cap);
 
     if (warp >= kMmaWarp) asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kMmaRegs));

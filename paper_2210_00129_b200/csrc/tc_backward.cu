@@ -85,7 +85,7 @@ constexpr uint32_t kBiasSmemBytes = kBiasThreads * 8 * sizeof(float) + kBiasChun
 constexpr int kEpiChunk = 16;            // accumulator columns (= rows of dW) per TMA store of the dW epilogue
 constexpr int kEpiBufs = 3;              // staging buffers the dW epilogue rotates through
 constexpr uint32_t kEpiBufBytes = kEpiChunk * kBM * sizeof(float);   // 8 KB: 16 rows of dW x 128 columns
-constexpr int kEpiBarrier = 2;           // named barrier of the four epilogue warps
+constexpr int kSideBarrier = 1, kEpiBarrier = 2;     // named barriers of the four side warps, of the four epilogue warps
 constexpr uint32_t kRingBytes = kStages * kStageBytes;
 static_assert(kRingBytes == kStagesNarrow * (kABytes + 128 * kRowBytes), "both ring shapes fill the same memory");
 constexpr uint32_t kSmemBytes = kRingBytes + 256 + kBiasSmemBytes + kEpiBufs * kEpiBufBytes + 1024;   // ring + control + bias + staging + slack
@@ -368,7 +368,11 @@ tc_backward_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
     int32_t* status_word = p.status_word;
 
     pdl_wait();                                                      // from here on global memory is read
-    const bool skip_all = status_word != nullptr && *reinterpret_cast<volatile int32_t*>(status_word) != 0;
+    bool skip_all = ptx::warp_sees_error(status_word);
+    if (status_word != nullptr) {
+        if (warp < 4) skip_all = ptx::bar_or<kEpiBarrier, 128>(skip_all);
+        else if (warp >= kGatherWarp0 && !is_gather_warp<kNarrow>(warp)) skip_all = ptx::bar_or<kSideBarrier, kBiasThreads>(skip_all);
+    }
     const int64_t M_keep = load_m_keep(p.M_keep_dev, p.M_keep_cap);
     const Schedule sched = make_schedule<BNX, BNW, kPair ? 2 * kBM : kBM>(p, M_keep);
     const int C_in = p.C_in, C_out = p.C_out;
@@ -653,7 +657,7 @@ tc_backward_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
                     // are under way meanwhile
                     ids[t] = id;
                     id = row_id(mc + kBiasChunk + t);
-                    asm volatile("bar.sync 1, %0;" ::"n"(kBiasThreads) : "memory");
+                    ptx::bar_named<kSideBarrier, kBiasThreads>();
                     if (cv < V) {
                         for (int r0 = rg; r0 < kBiasChunk && mc + r0 < m_end; r0 += RG * kBiasDepth) {
                             uint4 v[kBiasDepth];
@@ -674,12 +678,12 @@ tc_backward_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
                             }
                         }
                     }
-                    asm volatile("bar.sync 1, %0;" ::"n"(kBiasThreads) : "memory");
+                    ptx::bar_named<kSideBarrier, kBiasThreads>();
                 }
                 // add the row groups in a fixed order
 #pragma unroll
                 for (int e = 0; e < 8; ++e) red[t * 8 + e] = acc[e];
-                asm volatile("bar.sync 1, %0;" ::"n"(kBiasThreads) : "memory");
+                ptx::bar_named<kSideBarrier, kBiasThreads>();
                 if (rg == 0 && cv < V) {
                     float sum[8];
 #pragma unroll
@@ -691,7 +695,7 @@ tc_backward_kernel(const __grid_constant__ CUtensorMap map_w, const __grid_const
                     o[0] = make_float4(sum[0], sum[1], sum[2], sum[3]);
                     o[1] = make_float4(sum[4], sum[5], sum[6], sum[7]);
                 }
-                asm volatile("bar.sync 1, %0;" ::"n"(kBiasThreads) : "memory");
+                ptx::bar_named<kSideBarrier, kBiasThreads>();
             }
         }
     } else {

@@ -113,7 +113,8 @@ tc_forward_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
     int32_t* status_word = p.status_word;
 
     pdl_wait();
-    const bool skip_all = status_word != nullptr && *reinterpret_cast<volatile int32_t*>(status_word) != 0;
+    bool skip_all = ptx::warp_sees_error(status_word);
+    if (status_word != nullptr && warp < 4) skip_all = ptx::bar_or<kEpiBarrier, 128>(skip_all);
     const int C_in = p.C_in, C_out = p.C_out;
     const uint32_t ncol = (uint32_t)((C_out + BN - 1) / BN);
     constexpr int kTM = kPair ? 2 * kBM : kBM;                       // rows of a worker's tile

@@ -41,8 +41,35 @@ def ortho_calls(status):
     return calls
 
 
-@pytest.mark.parametrize("make", [norm_calls, ortho_calls])
-def test_a_word_that_changes_meanwhile(make):
+def layer_calls(status):
+    """Layers on the tensor cores (wide and narrow tiles, pairs of blocks), in fp32 both ways, and attention."""
+    calls = []
+    new = lambda *s, dtype=torch.bfloat16: torch.randn(s, device="cuda", generator=torch.Generator(device="cuda").manual_seed(len(calls))).to(dtype)
+    for dtype, code, M, C_in, C_out, flags in ((torch.bfloat16, 1, 12544, 768, 2304, 0), (torch.bfloat16, 1, 2000, 96, 384, 0),
+                                               (torch.bfloat16, 1, 2000, 64, 64, sbp.SBP_FLAG_W_OUT_IN), (torch.float32, 0, 2000, 768, 768, 0),
+                                               (torch.float32, 0, 2000, 64, 64, sbp.SBP_FLAG_PLAIN_FMA)):
+        keep = M // 2
+        rows = torch.arange(0, M, 2, dtype=torch.int32, device="cuda")
+        X, dY, W = new(M, C_in, dtype=dtype), new(M, C_out, dtype=dtype), new(C_in, C_out, dtype=dtype)
+        Xk, dX, Y = new(keep, C_in, dtype=dtype), new(M, C_in, dtype=dtype), new(M, C_out, dtype=dtype)
+        dW, db, bias = torch.empty(C_in, C_out, device="cuda"), torch.empty(C_out, device="cuda"), new(C_out, dtype=torch.float32)
+        nbytes = sbp.sbp_linear_backward_workspace_bytes(code, M, keep, C_in, C_out)
+        ws = torch.empty(nbytes, dtype=torch.uint8, device="cuda")
+        calls.append((lambda a=(code, X, W, bias, M, C_in, C_out, Y, None, None, 0, None, flags, status): sbp.sbp_linear_forward(*a), [Y]))
+        calls.append((lambda a=(code, Xk, dY, W, rows, None, M, keep, C_in, C_out, dW, db, dX, flags, ws, nbytes, status):
+                      sbp.sbp_linear_backward(*a), [dW, db, dX]))
+    B, N, heads = 8, 196, 4
+    Q, K, V, dA, dQ, dK, dV = (new(B * N, heads * 64) for _ in range(7))
+    offs = torch.arange(0, B * 98 + 1, 98, dtype=torch.int32, device="cuda")
+    tokens = torch.arange(0, B * N, 2, dtype=torch.int32, device="cuda")
+    calls.append((lambda a=(1, Q, K, V, heads * 64, dA, heads * 64, tokens, offs, tokens, offs, B, N, heads, 64, 98, dQ, dK, dV, heads * 64, 0,
+                            status): sbp.sbp_attention_backward(*a), [dQ, dK, dV]))
+    return calls
+
+
+# (warps of a layer's block that see the word change between them end at their waits' limit of two seconds: few rounds)
+@pytest.mark.parametrize("make,rounds,flips", [(norm_calls, 60, 30), (ortho_calls, 60, 30), (layer_calls, 3, 1)])
+def test_a_word_that_changes_meanwhile(make, rounds, flips):
     status = torch.zeros(1, dtype=torch.int32, device="cuda")
     calls = make(status)
     want = []
@@ -52,12 +79,12 @@ def test_a_word_that_changes_meanwhile(make):
     torch.cuda.synchronize()
     assert status.item() == 0
     work, other = torch.cuda.Stream(), torch.cuda.Stream()
-    for _ in range(60):
+    for _ in range(rounds):
         with torch.cuda.stream(work):
             for call, _ in calls:
                 call()
         with torch.cuda.stream(other):
-            for _ in range(2 * len(calls)):
+            for _ in range(flips):
                 status.fill_(sbp.SBP_ERR_BAD_INDICES)
                 status.zero_()
     torch.cuda.synchronize()
