@@ -346,6 +346,7 @@ sbp_status sbp_block_norm_backward(sbp_dtype dt, sbp_norm norm, const void* dR /
  *   out[m, :] = scale * table[ids[m], :] + add[m, :]         add [M, C] nullable (then + 0); out may be add
  * table [V, C], add, out [M, C] in dt, ids int32 [M].  A negative id means no row (padding: out = add, or zero).  An id of V
  * or more is reported as SBP_ERR_BAD_INDICES in the status word and taken as no row.  fp32 arithmetic, one rounding to dt.
+ * status_word as for sbp_linear_backward (an error that it holds before the call leaves out alone); it costs one more launch.
  * C * sizeof(element) must be a multiple of 16 (else SBP_ERR_UNSUPPORTED).  The other buffers do not overlap out.
  */
 sbp_status sbp_embedding_forward(sbp_dtype dt, const void* table /* dev */, int64_t V, int64_t C, const int32_t* ids /* dev */,
@@ -363,6 +364,7 @@ size_t sbp_embedding_backward_workspace_bytes(sbp_dtype dt, int64_t M_keep_cap, 
  * order; entries outside [0, M) are skipped.  Negative ids add nothing, ids of V or more are reported and add nothing.
  * Sums are fp32, each id's rows added in an order that depends on the sizes and the list alone: the same bits every time.
  * flags: SBP_FLAG_ACCUMULATE adds into dTable (rows without a k are not touched), SBP_FLAG_DY_COMPACT.
+ * status_word as for sbp_linear_backward (an error that it holds before the call leaves dTable alone); it costs one more launch.
  * workspace: 256-byte aligned; SBP_ERR_WORKSPACE if short.  V < 2^31, C as in the forward call.
  */
 sbp_status sbp_embedding_backward(sbp_dtype dt, const void* dOut /* dev */, const int32_t* ids /* dev */,

@@ -24,9 +24,10 @@ namespace {
 template <typename T, bool kAdd>
 __global__ void __launch_bounds__(kCopyThreads)
 embedding_forward_kernel(const uint4* __restrict__ table, const RowLength row, int64_t V, const int32_t* __restrict__ ids, int64_t M,
-                         float scale, const uint4* add, uint4* out, int32_t* status_word) {
+                         float scale, const uint4* add, uint4* out, const int32_t* status_word) {
     pdl_launch_dependents();
     pdl_wait();
+    if (block_sees_error(status_word)) return;
     const int64_t begin = (int64_t)blockIdx.x * kCopySpan, total = M * row.n;
     const SpanRows span(begin, row);
     int64_t src[kCopyUnroll];
@@ -39,8 +40,7 @@ embedding_forward_kernel(const uint4* __restrict__ table, const RowLength row, i
         src[u] = -1;
         if (begin + threadIdx.x + u * kCopyThreads < total) {
             const int64_t id = __ldg(ids + span.first + q);
-            if (id >= V) report_device_error(status_word, SBP_ERR_BAD_INDICES);
-            else if (id >= 0) src[u] = id * row.n + c;
+            if (id >= 0 && id < V) src[u] = id * row.n + c;
         }
     }
 #pragma unroll
@@ -64,6 +64,26 @@ embedding_forward_kernel(const uint4* __restrict__ table, const RowLength row, i
     }
 }
 
+// Reports ids of V or more among those of the kept rows, as a call's last launch: the kernels before it look whether an earlier call
+// left an error in the status word, and would stop at one of their own.  (Only with a status word; it adds 2 us to a call.)
+__global__ void __launch_bounds__(256) embedding_report_kernel(const int32_t* ids, const int32_t* keep_rows, const int32_t* M_keep_dev, int64_t M,
+                                                               int64_t M_keep_cap, int64_t V, int32_t* status_word) {
+    pdl_launch_dependents();
+    pdl_wait();
+    const int64_t n = load_m_keep(M_keep_dev, M_keep_cap);
+    for (int64_t m = (int64_t)blockIdx.x * 256 + threadIdx.x; m < n; m += (int64_t)gridDim.x * 256) {
+        const int32_t row = mapped_row(keep_rows, m);
+        if (row >= 0 && row < M && __ldg(ids + row) >= V) report_device_error(status_word, SBP_ERR_BAD_INDICES);
+    }
+}
+cudaError_t report_ids(const int32_t* ids, const int32_t* keep_rows, const int32_t* M_keep_dev, int64_t M, int64_t M_keep_cap, int64_t V,
+                       int32_t* status_word, cudaStream_t stream) {
+    if (status_word == nullptr || M_keep_cap == 0) return cudaSuccess;
+    const int64_t blocks = (M_keep_cap + 255) / 256, most = 8 * kNumSMs;
+    return launch_pdl(embedding_report_kernel, dim3((unsigned)(blocks < most ? blocks : most)), dim3(256), 0, stream, ids, keep_rows, M_keep_dev,
+                      M, M_keep_cap, V, status_word);
+}
+
 // ---- backward: the sort ----
 constexpr int kSortThreads = 512, kSortItems = 8, kSortTile = kSortThreads * kSortItems, kSortWarps = kSortThreads / 32;
 constexpr int kDigits = 256, kSortMaxBlocks = 128;
@@ -81,7 +101,7 @@ struct SortParams {
     int blocks, passes, bits;                         // sorting blocks; digits of `bits` bits
     uint4* clear;                                     // dTable, or nullptr
     int64_t clear_vecs;
-    int32_t* status_word;
+    const int32_t* status_word;
 };
 
 // Exclusive sums of one value a digit over the digits, by the first 256 threads; the others pass the barriers.
@@ -111,7 +131,7 @@ struct SortShared {
 // Blocks behind the sorting ones clear `part` of `parts` of dTable: one thread copies zeros from shared memory, 16 KB at a time, three
 // blocks an SM.  (12288 rows into 50257 x 768, the whole gradient: 41.4 us; two blocks an SM 49.7; stores by all threads 46 to 48.)
 __device__ __forceinline__ void clear_table(const SortParams& p, SortShared& sh, int part, int parts) {
-    if (p.clear == nullptr) return;
+    if (p.clear == nullptr || block_sees_error(p.status_word)) return;
     constexpr int64_t kPiece = sizeof(sh.count) / 16;
     const int64_t pieces = (p.clear_vecs + kPiece - 1) / kPiece, lo = pieces * part / parts, hi = pieces * (part + 1) / parts;
     for (int i = threadIdx.x; i < kSortWarps * kDigits; i += kSortThreads) (&sh.count[0][0])[i] = 0u;
@@ -141,21 +161,18 @@ __device__ __forceinline__ void count_digits(const SortParams& p, SortShared& sh
                 const int64_t at = tile + threadIdx.x + i * kSortThreads;
                 row[i] = at < end ? mapped_row(p.keep_rows, at) : -1;
             }
-            bool bad = false;
 #pragma unroll
             for (int i = 0; i < kSortItems; ++i) id[i] = __ldg(p.ids + (row[i] >= 0 && row[i] < p.M ? row[i] : 0));
 #pragma unroll
             for (int i = 0; i < kSortItems; ++i) {
                 const int64_t at = tile + threadIdx.x + i * kSortThreads;
                 const bool ok = row[i] >= 0 && row[i] < p.M;
-                bad |= ok && id[i] >= p.V;
                 key[i] = ok && id[i] >= 0 && id[i] < p.V ? (uint32_t)id[i] : (uint32_t)p.V;
                 if (at < end) {
                     p.keys[1][at] = key[i];
                     p.rows[1][at] = p.compact ? (int32_t)at : row[i];
                 }
             }
-            if (bad) report_device_error(p.status_word, SBP_ERR_BAD_INDICES);
         } else {
 #pragma unroll
             for (int i = 0; i < kSortItems; ++i) {
@@ -225,7 +242,8 @@ __device__ __forceinline__ void scatter_tile(const SortParams& p, SortShared& sh
     __syncthreads();
 }
 
-// The whole sort by the first cluster, which the others' clearing hides.
+// The whole sort by the first cluster, which the others' clearing hides.  (The sorting blocks write to the workspace alone, and do so
+// whatever the status word holds: the sums never see a list that is not sorted.)
 __global__ void __launch_bounds__(kSortThreads) embedding_sort_kernel(const SortParams p) {
     __shared__ SortShared sh;
     __shared__ uint32_t counts[kSortCluster][kDigits];               // of every block of the cluster
@@ -304,6 +322,7 @@ struct SumParams {
     float *dTable, *partial;                          // partial [pieces][2][C]: the id that came in from the left, the one that goes on
     int vecs, strips, piece, accumulate;              // 16-byte vectors of a row, 32-vector strips of it, places of a piece
     float scale;
+    const int32_t* status_word;
 };
 
 template <int P>
@@ -328,6 +347,7 @@ __global__ void __launch_bounds__(256) embedding_sum_kernel(const SumParams p) {
     constexpr int N = Vec<T>::N, P = N / 2;
     pdl_launch_dependents();
     pdl_wait();
+    if (block_sees_error(p.status_word)) return;
     const int lane = threadIdx.x & 31;
     const int64_t warp = (int64_t)blockIdx.x * 8 + (threadIdx.x >> 5);
     const int64_t piece = warp / p.strips;
@@ -397,6 +417,7 @@ __global__ void __launch_bounds__(256) embedding_join_kernel(const SumParams p) 
     __shared__ int64_t long_piece, long_end;
     pdl_launch_dependents();
     pdl_wait();
+    if (block_sees_error(p.status_word)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     if (threadIdx.x == 0) long_piece = -1;
     __syncthreads();
@@ -479,7 +500,7 @@ struct FewParams {
     float* dTable;
     int vecs, compact, accumulate;
     float scale;
-    int32_t* status_word;
+    const int32_t* status_word;
 };
 
 template <typename T>
@@ -491,6 +512,7 @@ __global__ void __launch_bounds__(256) embedding_few_kernel(const FewParams p) {
     __shared__ f32x2 part[8][32][P + 1];
     pdl_launch_dependents();
     pdl_wait();
+    if (block_sees_error(p.status_word)) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int n = (int)load_m_keep(p.M_keep_dev, p.M_keep_cap), mine = (int)blockIdx.x;
     const bool clears = mine >= (int)p.M_keep_cap;
@@ -506,7 +528,6 @@ __global__ void __launch_bounds__(256) embedding_few_kernel(const FewParams p) {
         for (int i = 0; i < kFewRows / 256; ++i) {
             const int m = (int)threadIdx.x + i * 256;
             const bool ok = row[i] >= 0 && row[i] < p.M;
-            if (m == mine && ok && id[i] >= p.V) report_device_error(p.status_word, SBP_ERR_BAD_INDICES);
             keys[m] = ok && id[i] >= 0 && id[i] < p.V ? (uint32_t)id[i] : 0xffffffffu;
             rows[m] = p.compact ? m : row[i];
         }
@@ -633,7 +654,8 @@ cudaError_t launch_embedding_forward(sbp_dtype dt, const void* table, int64_t V,
     const RowLength row(vecs);
     const dim3 grid((unsigned)copy_blocks(M * vecs)), block(kCopyThreads);
     auto go = [&](auto kernel) {
-        return launch_pdl(kernel, grid, block, 0, stream, (const uint4*)table, row, V, ids, M, scale, (const uint4*)add, (uint4*)out, status_word);
+        const cudaError_t e = launch_pdl(kernel, grid, block, 0, stream, (const uint4*)table, row, V, ids, M, scale, (const uint4*)add, (uint4*)out, status_word);
+        return e == cudaSuccess ? report_ids(ids, nullptr, nullptr, M, M, V, status_word, stream) : e;
     };
     if (dt == SBP_BF16) return add ? go(embedding_forward_kernel<__nv_bfloat16, true>) : go(embedding_forward_kernel<__nv_bfloat16, false>);
     return add ? go(embedding_forward_kernel<float, true>) : go(embedding_forward_kernel<float, false>);
@@ -647,6 +669,7 @@ size_t embedding_backward_workspace_bytes(sbp_dtype dt, int64_t M_keep_cap, int6
 cudaError_t launch_embedding_backward(sbp_dtype dt, const void* dOut, bool compact, const int32_t* ids, const int32_t* keep_rows,
                                       const int32_t* M_keep_dev, int64_t M, int64_t M_keep_cap, int64_t V, int64_t C, float scale,
                                       float* dTable, bool accumulate, void* workspace, int32_t* status_word, cudaStream_t stream) {
+    auto reported = [&](cudaError_t e) { return e == cudaSuccess ? report_ids(ids, keep_rows, M_keep_dev, M, M_keep_cap, V, status_word, stream) : e; };
     if (M_keep_cap <= kFewRows && M_keep_cap <= 32 * V) {
         FewParams f = {};
         f.dOut = (const uint4*)dOut;
@@ -665,8 +688,8 @@ cudaError_t launch_embedding_backward(sbp_dtype dt, const void* dOut, bool compa
         const int64_t clear = accumulate ? 0 : (V + 7) / 8 < 4 * kNumSMs ? (V + 7) / 8 : 4 * kNumSMs;
         if (M_keep_cap + clear == 0) return cudaSuccess;             // nothing to add, and nothing to clear
         const dim3 grid((unsigned)(M_keep_cap + clear));
-        return dt == SBP_BF16 ? launch_pdl(embedding_few_kernel<__nv_bfloat16>, grid, dim3(256), 0, stream, f)
-                              : launch_pdl(embedding_few_kernel<float>, grid, dim3(256), 0, stream, f);
+        return reported(dt == SBP_BF16 ? launch_pdl(embedding_few_kernel<__nv_bfloat16>, grid, dim3(256), 0, stream, f)
+                                       : launch_pdl(embedding_few_kernel<float>, grid, dim3(256), 0, stream, f));
     }
     const SortShape so = sort_shape(M_keep_cap, V);
     const SumShape su = sum_shape(dt, M_keep_cap, C);
@@ -721,13 +744,15 @@ cudaError_t launch_embedding_backward(sbp_dtype dt, const void* dOut, bool compa
     s.piece = su.piece;
     s.accumulate = accumulate;
     s.scale = scale;
+    s.status_word = status_word;
     const int64_t warps = su.pieces * su.strips;
     const dim3 sum_grid((unsigned)((warps + 7) / 8)), join_grid((unsigned)((su.pieces + 7) / 8 * su.strips));
     e = dt == SBP_BF16 ? launch_pdl(embedding_sum_kernel<__nv_bfloat16>, sum_grid, dim3(256), 0, stream, s)
                        : launch_pdl(embedding_sum_kernel<float>, sum_grid, dim3(256), 0, stream, s);
-    if (e != cudaSuccess || su.pieces < 2) return e;
-    return dt == SBP_BF16 ? launch_pdl(embedding_join_kernel<__nv_bfloat16>, join_grid, dim3(256), 0, stream, s)
-                          : launch_pdl(embedding_join_kernel<float>, join_grid, dim3(256), 0, stream, s);
+    if (e == cudaSuccess && su.pieces >= 2)
+        e = dt == SBP_BF16 ? launch_pdl(embedding_join_kernel<__nv_bfloat16>, join_grid, dim3(256), 0, stream, s)
+                           : launch_pdl(embedding_join_kernel<float>, join_grid, dim3(256), 0, stream, s);
+    return reported(e);
 }
 
 }  // namespace sbp
