@@ -289,7 +289,8 @@ sbp_status sbp_act_backward(sbp_dtype dt, sbp_activation act, const void* Z_keep
  * Outputs: R [M, C] (nullable; may be H or Y), Z [M, C] (nullable), and the packed rows Y_keep, R_keep, Z_keep
  * [M_keep_cap, C] (each nullable) of Y, R and Z with the rows past M_keep cleared: R_keep and Y_keep are what
  * sbp_block_norm_backward reads, Z_keep is the X_keep of the linear layer behind the norm.  keep_rows strictly ascending,
- * as sbp_sample_keep writes them; NULL: rows 0 .. M_keep - 1.  M_keep as for sbp_forward_cache.
+ * as sbp_sample_keep writes them; NULL: rows 0 .. M_keep - 1; entries outside [0, M) have cleared rows.  M_keep as for
+ * sbp_forward_cache.
  * No buffer overlaps another, but for R.  Statistics and sums in fp32; R is normalised before it is rounded; one rounding
  * to dt of each output.
  * SBP_ERR_UNSUPPORTED: C * sizeof(element) not a multiple of 16, C > 8192.  SBP_ERR_INVALID_ARG for null / misaligned (16

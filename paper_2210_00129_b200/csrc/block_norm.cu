@@ -34,6 +34,26 @@ struct NormFwdParams {
     int caches;
 };
 
+// Rows of the caches past M_keep are cleared, and those of entries outside the tensor, the first or the last ones of the list: by worker
+// `worker` of `workers`, `threads` threads.  (A function of its own, so that it takes no registers from the rows: inlined it cost up to 4 %.)
+__device__ __noinline__ void clear_cache_rows(uint4* Y_keep, uint4* R_keep, uint4* Z_keep, const int32_t* keep_rows, int64_t M, int64_t M_keep,
+                                              int64_t M_keep_cap, int vecs, int64_t worker, int64_t workers, int t, int threads) {
+    const uint4 zero = make_uint4(0u, 0u, 0u, 0u);
+    auto clear = [&](int64_t m) {
+        for (int v = t; v < vecs; v += threads) {
+            if (Y_keep != nullptr) Y_keep[m * vecs + v] = zero;
+            if (R_keep != nullptr) R_keep[m * vecs + v] = zero;
+            if (Z_keep != nullptr) Z_keep[m * vecs + v] = zero;
+        }
+    };
+    for (int64_t m = M_keep + worker; m < M_keep_cap; m += workers) clear(m);
+    if (keep_rows == nullptr) return;
+    if (worker == 0)
+        for (int64_t m = 0; m < M_keep && keep_rows[m] < 0; ++m) clear(m);
+    if (worker == workers - 1)
+        for (int64_t m = M_keep - 1; m >= 0 && keep_rows[m] >= M; --m) clear(m);
+}
+
 // kLanes threads of a warp share a row (kLanes 0: a block, for long rows), each with kNV vectors of it, kU rows at a time; the rows of a
 // warp, `chunk` <= 32 consecutive ones, are dealt to its groups of lanes in turn.  Which of them are kept, and the place of each in
 // the caches, comes from one search of the list.  kFull: the threads' vectors are the row's, none lies behind it (what those
@@ -203,15 +223,9 @@ norm_forward_kernel(const NormFwdParams p) {
             __syncwarp();
         }
     }
-    // rows past M_keep of the caches are cleared
-    if (p.caches) {
-        for (int64_t m = M_keep + worker; m < p.M_keep_cap; m += workers)
-            for (int v = kMulti ? (int)threadIdx.x : lane; v < p.vecs; v += kMulti ? (int)blockDim.x : 32) {
-                if (p.Y_keep != nullptr) p.Y_keep[m * p.vecs + v] = zero;
-                if (p.R_keep != nullptr) p.R_keep[m * p.vecs + v] = zero;
-                if (p.Z_keep != nullptr) p.Z_keep[m * p.vecs + v] = zero;
-            }
-    }
+    // (kLanes 0: the threads of the block)
+    if (p.caches) clear_cache_rows(p.Y_keep, p.R_keep, p.Z_keep, p.keep_rows, p.M, M_keep, p.M_keep_cap, p.vecs, worker, workers,
+                                   kMulti ? (int)threadIdx.x : lane, kMulti ? (int)blockDim.x : 32);
 }
 
 // ---- backward ----
