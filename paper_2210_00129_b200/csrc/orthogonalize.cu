@@ -934,7 +934,8 @@ __device__ __forceinline__ void inverse_norm(double norm, float& power, float& f
     int e = norm > 0.0 && isfinite(norm) ? ilogb(norm) : 0;
     e = e > 126 ? 126 : e < -126 ? -126 : e;
     power = scalbnf(1.f, -e);
-    factor = (float)(4096.0 / ldexp(norm, -e));
+    const double f = 4096.0 / ldexp(norm, -e);
+    factor = norm > 0.0 && f > 3e38 ? 3e38f : (float)f;              // (an eps below 2^-149, alone: of zeros, which stay zeros)
 }
 
 // ---- the start: momentum, the norm, the two fp16 numbers of U / (|U| + eps) ----
