@@ -19,8 +19,10 @@
 // All products of a call run in one launch of a persistent kernel.  Its items are the tiles of all products of all matrices, in the
 // order step, product, matrix, tile; blocks draw the next one from a counter, and an item waits until the tiles of its matrix
 // that it depends on are done (a count for each matrix).  Items only wait for items drawn before them, so some block can always
-// go on, however many are resident; with several matrices nothing waits, and the epilogue of one tile runs under the products of
-// the next.  (One launch a product, seventeen a call, cost 8 us each before their first tile.)  Operands come by TMA, X in either
+// go on, however many are resident.  With several matrices the tiles of others, and the products under an epilogue, hide part of
+// the 7 us from a tile's stores to the first product that reads them, but not all of it: the chain of dependent products is the
+// bound (12 of 768 x 768: 3 us of products a tile).  (One launch a product, seventeen a call, cost 8 us each before their first
+// tile.)  Operands come by TMA, X in either
 // orientation as it lies; tcgen05.mma into accumulators in turns; the epilogue forms the next operand from the sums.  A and B
 // are symmetric: only tiles on and above the diagonal are made, and stored both ways.
 #include "tc_ptx.cuh"
@@ -1511,8 +1513,9 @@ OrthoLayout ortho_layout(sbp_dtype dt, int64_t count, int64_t rows, int64_t cols
     const int64_t want = (rows * cols / 4 + 4 * kStartThreads - 1) / (4 * kStartThreads), most = kStartBlocks / count > 1 ? kStartBlocks / count : 1;
     l.start_blocks = (int)(want < 1 ? 1 : want < most ? want : most);
     // 256 wide tiles take half as much of their operands from the L2 for a product, but there are half as many: from about three 128
-    // wide ones an SM on (4 x 2048 x 2048, 1024 of them: 730 us, 833 with 128; 512: 499 and 537; 24 x 768 x 768, 864: 374 and 394;
-    // 12 x 768 x 768, 432: 237 and 222; 4 x 2304 x 768, 432: 274 and 229; 8 x 1261 x 222, 160: 226 and 189)
+    // wide ones an SM on.  (Whole calls without momentum, 256 wide and 128 wide, us: 4 x 2048 x 2048, 1024 tiles of 128, 705 and 818;
+    // 24 x 768 x 768, 864, 380 and 397; 2 x 2048 x 2048, 512, 499 and 492 to 520; 12 x 768 x 768, 432, 231 and 219; 4 x 2304 x 768,
+    // 432, 274 and 242; 8 x 1261 x 222, 160, 254 to 300 and 236.)
     l.width = !l.exact && (rows + kTile - 1) / kTile * ((cols + kTile - 1) / kTile) * count > 3 * kNumSMs ? 256 : 128;
     const uint32_t tiles = (uint32_t)((l.m + kTile - 1) / kTile), wide = (uint32_t)((l.m + l.width - 1) / l.width), f = (uint32_t)l.width / kTile;
     l.sym_tiles = f * wide * (wide + 1) / 2 - (f * wide - tiles);
@@ -1547,7 +1550,9 @@ cudaError_t launch_products(const CUtensorMap& x_rows, const CUtensorMap& x_acro
 
 // Blocks of a matrix's cluster, and the positions of the longer side each has; 0 where the other kernels take the matrix.  A step is
 // 6.5 us without other blocks (128 positions; 10 with 256) and 12.4 with: 100 x 257, momentum included, 80 us on four blocks and 89
-// on two, 100 x 256 67 us on one and 71 on two.
+// on two, 100 x 256 67 us on one and 71 on two.  Without momentum, one matrix and twenty: 100 x 256 66 and 66 us on one block, 73 and 155
+// on eight; 100 x 400 73 and 77 on four, 73 and 156 on eight; 100 x 513 85 and 179 on eight, 93 and 97 on four; 100 x 1000 80 and 169
+// on eight, 93 and 99 on four (eight blocks a matrix fill the device twice from 19 matrices on: the rule is made for few).
 int ortho_small_blocks(int64_t n) { return n <= 256 ? 1 : n <= 512 ? 4 : 8; }
 int ortho_small_slice(int64_t rows, int64_t cols) {
     const int64_t m = rows < cols ? rows : cols, n = rows < cols ? cols : rows;
