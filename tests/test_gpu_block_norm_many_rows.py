@@ -67,3 +67,29 @@ def test_entries_outside_the_tensor_among_a_workers_rows(dtype, M, C, keep, grou
 @pytest.mark.parametrize("kind,post,bias,group", base.VARIANTS)
 def test_forward_chunks_of_several_rows(dtype, M, C, keep, kind, post, bias, group):
     base.test_forward(dtype, M, C, keep, kind, post, bias, group)
+
+
+def test_calls_at_once_on_three_streams():
+    shapes = [("bf16", 6000, 768, 3000), ("f32", 9000, 128, 4500), ("bf16", 1500, 4096, 1500)]
+    made = [base.inputs(d, M, C, keep, True, True, 50) for d, M, C, keep in shapes]
+    fwd = [base.run_forward(d, 0, s, M, C, keep) for s, (d, M, C, keep) in zip(made, shapes)]
+    bwd = [base.run_backward(d, 0, s, M, C, keep) for s, (d, M, C, keep) in zip(made, shapes)]
+    streams = [torch.cuda.Stream() for _ in shapes]
+    outs, spaces = [], []
+    for s, f, o, (d, M, C, keep) in zip(made, fwd, bwd, shapes):
+        outs.append({n: torch.full_like(t, float("nan")) for n, t in (f | o).items()})
+        spaces.append(torch.empty(sbp.sbp_block_norm_backward_workspace_bytes(base.DT[d][0], M, keep, C), dtype=torch.uint8, device="cuda"))
+    torch.cuda.synchronize()
+    for _ in range(4):
+        for s, o, ws, stream, (d, M, C, keep) in zip(made, outs, spaces, streams, shapes):
+            code = base.DT[d][0]
+            with torch.cuda.stream(stream):
+                sbp.sbp_block_norm_forward(code, 0, s["H"], s["Y"], s["post_w"], s["post_b"], s["gate"], s["group"], 0.9, s["pre_w"], s["pre_b"],
+                                           base.EPS, M, C, o["R"], o["Z"], s["rows"], None, keep, o["Y_keep"], o["R_keep"], o["Z_keep"])
+                sbp.sbp_block_norm_backward(code, 0, s["dR"], s["dZ"], s["R"], s["Yk"], s["post_w"], s["post_b"], s["gate"], s["group"], 0.9,
+                                            s["pre_w"], base.EPS, s["rows"], None, M, keep, C, o["dH"], o["dY"], o["dpost_w"], o["dpost_b"],
+                                            o["dgate"], o["dpre_w"], o["dpre_b"], 0, ws, ws.numel())
+    torch.cuda.synchronize()
+    for o, f, b in zip(outs, fwd, bwd):
+        for n, want in (f | b).items():
+            assert torch.equal(o[n], want), n
