@@ -392,7 +392,8 @@ size_t sbp_orthogonalize_workspace_bytes(sbp_dtype dt, int64_t count, int64_t ro
  * Precision: the norm in 64 bits; X as two fp16 numbers (22 bits) wherever it carries a direction on, products on the
  * tensor cores with fp32 sums.  SBP_BF16: operands of the products in fp16, but for the diagonals of A and of its
  * polynomial (fp32) - about 1e-3 of the result's norm, against 1.7e-3 that the rounding of O to bf16 brings; sides up to
- * 128, and SBP_F32: both fp16 numbers in the products (three instead of one), about 1e-6 of the norm.  What is smaller than
+ * 128, and SBP_F32: both fp16 numbers in the products (three instead of one), as near to 64 bits as the iteration in fp32
+ * is, 1e-6 to 2e-6 of the norm after five steps (gradients of few directions: 1e-5).  What is smaller than
  * 2^-23 of the largest numbers of U may show, grown by a factor of up to a ^ steps, in directions where U has none.
  * A matrix of zeros gives zeros (with eps = 0: NaN); infinite and NaN gradients give NaN in their matrix.
  * SBP_ERR_INVALID_ARG for null or misaligned (16 bytes) pointers, sizes below 1, steps outside 1 .. 32, beta, eps or scale not

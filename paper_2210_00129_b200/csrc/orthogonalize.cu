@@ -12,8 +12,11 @@
 // The diagonals of A and B carry most of what the products weigh and stay in fp32 beside them.  That leaves 1e-3 of the norm,
 // half of what rounding the result to bf16 adds (512 x 512 normal: 0.75e-3; all products in bf16: 1e-2).  Results in fp32,
 // and matrices with a side up to kExactSide (whose few roundings do not average out), take both numbers of every operand:
-// three products instead of one, 1e-6.  There the tensor core's running sum, which it cuts short instead of rounding (7e-8 of
-// it for each 64 deep block), is read out every kPartBlocks blocks and added up in fp32 registers, the small products first.
+// three products instead of one: no further from 64 bits than the iteration in fp32 (533 x 1926 normal: 1.5e-6 and 3.3e-6 of the
+// norm after five steps; rank 20: 1.5e-5 and 3.0e-5).  There the tensor core's running sum, which it cuts short instead of rounding
+// (7e-8 of it for each 64 deep block), is read out every four blocks and added up in fp32 registers, the small products first.  On
+// the diagonals of A and A^2 all terms have one sign, the cuts add up, and the steps grow what they leave (8.3e-6): the tiles there
+// are read out twice a block (2 x 4096 x 1024 574 us -> 590; once a block 573 and 2.4e-6).
 // X, A and B are held times 2^12, which keeps the small numbers of large matrices out of fp16's subnormals.
 //
 // All products of a call run in one launch of a persistent kernel.  Its items are the tiles of all products of all matrices, in the
@@ -37,7 +40,6 @@ namespace {
 constexpr float kNsA = 3.4445f, kNsB = -4.7750f, kNsC = 2.0315f;
 constexpr float kUp = 4096.f, kDown = 1.f / 4096.f;                 // X, A and B are held times 2^12
 constexpr int kExactSide = 128;
-constexpr int kPartBlocks = 4;
 
 constexpr int kTile = 128, kDeep = 64, kUmmaDeep = 16;               // rows of a tile, depth of a stage and of an instruction
 constexpr uint32_t kRow = 128;                                      // bytes of a 64 deep row
@@ -50,6 +52,8 @@ constexpr uint32_t kOrthoSmem = kRing + kControl + kStagingBytes + 1024;
 constexpr int kMostStages = 6, kItems = 4;
 
 enum { kGram = 0, kPoly = 1, kStep = 2 };
+// 16 deep products whose sum is read out together where both numbers of every operand are taken: two on the diagonal of A and its square
+__device__ __forceinline__ int part_products(int mode, int i, int j) { return mode != kStep && i == j ? 2 : 16; }
 
 struct alignas(16) OrthoControl {
     uint64_t full[kMostStages], empty[kMostStages];                  // a stage's operands: in place, read
@@ -358,7 +362,7 @@ __device__ __forceinline__ bool ortho_epilogue_exact(const OrthoParams& p, const
     for (int i = 0; i < kCols; ++i) sum[i] = 0.f;
     {
         int from_block;
-        const int blocks = ortho_blocks(p, t, from_block);
+        const int products = ortho_blocks(p, t, from_block) * (kDeep / kUmmaDeep), each = part_products(kMode, t.i, t.j);
         auto add = [&](uint32_t taddr) {
 #pragma unroll
             for (int c = 0; c < kCols; c += 32) {
@@ -369,7 +373,7 @@ __device__ __forceinline__ bool ortho_epilogue_exact(const OrthoParams& p, const
                 for (int i = 0; i < 32; ++i) sum[c + i] += v[i];
             }
         };
-        for (int part = 0; part < blocks; part += kPartBlocks) {
+        for (int part = 0; part < products; part += each) {
             if (!take_sums(w, w.ctl->acc_full, w.acc, p.status_word)) return false;
             add(w.tmem + w.acc.slot() * kWidth + w.half * kCols);
             give_back(w, w.ctl->acc_empty, w.acc);
@@ -806,6 +810,7 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
             const bool with_extras = !kExact && t.mode == kStep;
             int from;
             const int blocks = ortho_blocks(p, t, from) + (with_extras ? step_extras<kWidth>(p) : 0);
+            const int each = part_products(t.mode, t.i, t.j), last_product = blocks * (kDeep / kUmmaDeep) - 1;
             const uint32_t idesc = ptx::umma_idesc_f16(kTile, kWidth, across_a, across_b);
             const uint32_t a_step = (across_a ? kUmmaDeep * kRow : kUmmaDeep * 2u) >> 4, b_step = (across_b ? kUmmaDeep * kRow : kUmmaDeep * 2u) >> 4;
             const uint32_t a_lo = ptx::umma_desc_lo(ring, across_a ? kHalfOperand : 16u);
@@ -816,24 +821,35 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
             };
             if (kExact) ok = wait_empty(ctl->small_empty, small);
             for (int k = 0; k < blocks && ok; ++k, ++it) {
-                const bool fresh = kExact ? k % kPartBlocks == 0 : k == 0;
-                if (fresh && !(ok = wait_empty(ctl->acc_empty, acc))) break;
+                if (!kExact && k == 0 && !(ok = wait_empty(ctl->acc_empty, acc))) break;
                 const uint32_t s = it % kStages;
                 ok = ptx::mbar_wait(ptx::smem_addr(&ctl->full[s]), (it / kStages) & 1u, abort_flag, status_word);
                 ok = __all_sync(0xffffffffu, ok);
                 if (!ok) break;
                 ptx::tc_fence_after_sync();
-                const uint32_t a = a_lo + s * (kStage >> 4), b = b_lo + s * (kStage >> 4), d = tmem + acc.slot() * kWidth;
+                const uint32_t a = a_lo + s * (kStage >> 4), b = b_lo + s * (kStage >> 4);
                 if constexpr (kExact) {
                     const uint32_t d2 = tmem + (2 + small.slot()) * kWidth, two = kPlane >> 4;
 #pragma unroll
                     for (uint32_t u = 0; u < kDeep / kUmmaDeep; ++u) {
-                        const uint32_t au = a + u * a_step, bu = b + u * b_step;
+                        const int at = k * (int)(kDeep / kUmmaDeep) + (int)u;
+                        const bool fresh = (at & (each - 1)) == 0;
+                        if (fresh) {
+                            if (!(ok = wait_empty(ctl->acc_empty, acc))) break;
+                            ptx::tc_fence_after_sync();
+                        }
+                        const uint32_t au = a + u * a_step, bu = b + u * b_step, d = tmem + acc.slot() * kWidth;
                         ptx::umma_bf16_warp<false>(d2, ptx::umma_desc_of(au + two), ptx::umma_desc_of(bu), idesc, (k | u) != 0u, leader);
-                        ptx::umma_bf16_warp<false>(d, ptx::umma_desc_of(au), ptx::umma_desc_of(bu), idesc, !(fresh && u == 0u), leader);
+                        ptx::umma_bf16_warp<false>(d, ptx::umma_desc_of(au), ptx::umma_desc_of(bu), idesc, !fresh, leader);
                         ptx::umma_bf16_warp<false>(d2, ptx::umma_desc_of(au), ptx::umma_desc_of(bu + two), idesc, true, leader);
+                        if ((at & (each - 1)) == each - 1 || at == last_product) {
+                            if (leader) ptx::umma_commit(ptx::smem_addr(&ctl->acc_full[acc.slot()]));
+                            ++acc.used;
+                        }
                     }
+                    if (!ok) break;
                 } else {
+                    const uint32_t d = tmem + acc.slot() * kWidth;
                     const int narrow = with_extras ? step_block<kWidth>(p, t, k).narrow : 0;
                     const uint32_t di = narrow ? d + kTile * (narrow - 1) : d, id = narrow ? ptx::umma_idesc_f16(kTile, kTile, false, false) : idesc;
 #pragma unroll
@@ -841,7 +857,7 @@ ortho_kernel(const __grid_constant__ CUtensorMap x_rows, const __grid_constant__
                         ptx::umma_bf16_warp<false>(di, ptx::umma_desc_of(a + u * a_step), ptx::umma_desc_of(b + u * b_step), id, (k | u) != 0u, leader);
                 }
                 if (leader) ptx::umma_commit(ptx::smem_addr(&ctl->empty[s]));
-                if (k == blocks - 1 || (kExact && k % kPartBlocks == kPartBlocks - 1)) {
+                if (!kExact && k == blocks - 1) {
                     if (leader) ptx::umma_commit(ptx::smem_addr(&ctl->acc_full[acc.slot()]));
                     ++acc.used;
                 }
@@ -1088,7 +1104,8 @@ __global__ void __launch_bounds__(kStartThreads) ortho_scale_kernel(const StartP
 // reduction-major operand of A and, unchanged, the other operand of B X (a tall matrix is turned when it is read).  A's partial
 // sums over the slices go to the blocks that own their rows, and A comes back to all of them, through distributed shared memory;
 // everything else stays in the block.  Momentum and norm included, it is one launch without a wait on another cluster.
-// Both fp16 numbers of every operand, as the other exact products; no chain of products is longer than four blocks here.
+// Both fp16 numbers of every operand, as the other exact products.  A's sums and those of its square go to three accumulators in turns,
+// which are added up in fp32: 100 x 257 81.5 us, error 0.8e-6; one accumulator 78.9 us, 1.7e-6 (the iteration in fp32: 1.5e-6).
 constexpr int kSmallSide = 128, kSmallSlice = 256, kSmallCluster = 8, kSmallThreads = 512;
 constexpr uint32_t kSmallBlock = 128 * kRow;                        // 128 x 64 numbers
 constexpr uint32_t kSmallX = 4 * kSmallBlock, kSmallS = 2 * kSmallBlock;         // a plane of X, of A and B
@@ -1265,13 +1282,15 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const Sma
     const uint32_t lane_tmem = tmem + ((uint32_t)(quad * 32) << 16);
     // tensor memory: A and its polynomial in columns 0 .. 127, the next X in 256 ..; the small products of the three, first x second
     // and second x first, 128 columns further on (an instruction that adds to the place of the one before it waits for it),
-    // where a slice of over 128 positions does not need them
+    // where a slice of over 128 positions does not need them.  A and its square use the next X's columns too: their products go to three
+    // places in turns (see the head: short chains).
     const bool narrow = p.slice <= 128;
-    const uint32_t d_sym = 0, d_step = 256;
+    const uint32_t d_sym = 0, d_step = 256, d_more = 256;
     const int m16 = (p.m + 15) / 16 * 16, deep_m = (p.m + kDeep - 1) / kDeep, deep_n = p.slice / kDeep;
     uint32_t phase = 0;
     // products of a and b (reduction along their rows, or down b's: across), the small ones to `two` where that is another place
-    auto multiply = [&](uint32_t d, uint32_t two, uint32_t a, uint32_t a_plane, uint32_t b, uint32_t b_plane, bool across, int width_n, int blocks_k) {
+    auto multiply = [&](bool symmetric, uint32_t d, uint32_t two, uint32_t a, uint32_t a_plane, uint32_t b, uint32_t b_plane, bool across, int width_n,
+                        int blocks_k) {
         asm volatile("fence.proxy.async;" ::: "memory");             // what this thread wrote to shared memory, for the tensor core
         ptx::tc_fence_before_sync();
         __syncthreads();
@@ -1280,18 +1299,23 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const Sma
             const bool leader = ptx::elect_one();
             const uint32_t idesc = ptx::umma_idesc_f16(kTile, width_n, false, across);
             const uint32_t a_lo = ptx::umma_desc_lo(a, 16u), b_lo = ptx::umma_desc_lo(b, across ? kSmallBlock : 16u);
+            uint32_t place_at = 0u;
 #pragma unroll 1
-            for (int k = 0; k < blocks_k; ++k)
+            for (int k = 0; k < blocks_k; ++k) {
 #pragma unroll
                 for (uint32_t u = 0; u < kDeep / kUmmaDeep; ++u) {
                     // along: 32 bytes of a row, the next 64 in the next block; across: 16 rows down, 64 rows in a deep block
                     const uint32_t au = a_lo + ((k * kSmallBlock + u * kUmmaDeep * 2) >> 4);
                     const uint32_t bu = b_lo + ((across ? k * kHalfOperand + u * kUmmaDeep * kRow : k * kSmallBlock + u * kUmmaDeep * 2) >> 4);
                     const bool more = k != 0 || u != 0u;
+                    const bool fresh = k == 0 && u < (symmetric ? 3u : 1u);
+                    const uint32_t dk = tmem + d + place_at;
+                    if (symmetric) place_at = place_at == 0u ? d_more : place_at == d_more ? d_more + 128u : 0u;
                     ptx::umma_bf16_warp<false>(tmem + two, ptx::umma_desc_of(au + (a_plane >> 4)), ptx::umma_desc_of(bu), idesc, more, leader);
-                    ptx::umma_bf16_warp<false>(tmem + d, ptx::umma_desc_of(au), ptx::umma_desc_of(bu), idesc, more || two == d, leader);
+                    ptx::umma_bf16_warp<false>(dk, ptx::umma_desc_of(au), ptx::umma_desc_of(bu), idesc, !fresh || two == d, leader);
                     ptx::umma_bf16_warp<false>(tmem + two, ptx::umma_desc_of(au), ptx::umma_desc_of(bu + (b_plane >> 4)), idesc, true, leader);
                 }
+            }
             if (leader) ptx::umma_commit(ptx::smem_addr(&product_done));
             __syncwarp();
         }
@@ -1312,6 +1336,20 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const Sma
             ptx::tmem_ld_wait();
         }
     };
+    auto symmetric_sums = [&](float (&v)[32]) {                      // 32 columns from cols0 on
+#pragma unroll
+        for (int h = 0; h < 32; h += 16) {
+            float w[4][16];
+            const uint32_t from = lane_tmem + d_sym + cols0 + h;
+            ptx::tmem_ld_32x16(from, w[0]);
+            ptx::tmem_ld_32x16(from + d_more, w[1]);
+            ptx::tmem_ld_32x16(from + d_more + 128, w[2]);
+            ptx::tmem_ld_32x16(from + 128, w[3]);
+            ptx::tmem_ld_wait();
+#pragma unroll
+            for (int e = 0; e < 16; ++e) v[h + e] = ((w[0][e] + w[1][e]) + w[2][e]) + w[3][e];
+        }
+    };
     // 32 numbers of a row, times 2^12, as two fp16 numbers each
     auto put = [&](uint8_t* plane, uint32_t second, int r, int c, float (&v)[32]) {
 #pragma unroll
@@ -1323,9 +1361,9 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const Sma
     };
     for (int step = 0; step < p.steps; ++step) {
         // A: every block's share of the sum
-        multiply(d_sym, d_sym + 128, x_addr, kSmallX, x_addr, kSmallX, false, m16, deep_n);
+        multiply(true, d_sym, d_sym + 128, x_addr, kSmallX, x_addr, kSmallX, false, m16, deep_n);
         float v[32];
-        sums(d_sym + cols0, d_sym + 128 + cols0, v);
+        symmetric_sums(v);
 #pragma unroll
         for (int e = 0; e < 32; ++e) v[e] = cols0 + e < m16 ? v[e] * kDown : 0.f;      // (columns that no product wrote)
         if (blocks == 1) {
@@ -1389,8 +1427,8 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const Sma
             ptx::cluster_sync_all();
         }
         // B = b A + c A^2, its diagonal apart in fp32
-        multiply(d_sym, d_sym + 128, s_addr, kSmallS, s_addr, kSmallS, false, m16, deep_m);
-        sums(d_sym + cols0, d_sym + 128 + cols0, v);
+        multiply(true, d_sym, d_sym + 128, s_addr, kSmallS, s_addr, kSmallS, false, m16, deep_m);
+        symmetric_sums(v);
         const float d = diag_a[row];
         float on_diagonal = 0.f;
 #pragma unroll
@@ -1414,7 +1452,7 @@ __global__ void __launch_bounds__(kSmallThreads, 1) ortho_small_kernel(const Sma
         put(S, kSmallS, row, cols0, v);
         // X <- a X + B X
         const uint32_t d_two = narrow ? d_step + 128 : d_step;
-        multiply(d_step, d_two, s_addr, kSmallS, x_addr, kSmallX, true, p.slice, deep_m);
+        multiply(false, d_step, d_two, s_addr, kSmallS, x_addr, kSmallX, true, p.slice, deep_m);
         const float f = kNsA + diag_b[row];
         const bool last = step == p.steps - 1;
         if (blocks > 1 && !narrow && !last) asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
